@@ -1,0 +1,274 @@
+// Writes to and reads from the paged cache: cache_append, cache_keep,
+// cache_read.  All are bound by memory (and, for a few tokens, by the launch):
+// DIM / 8 lanes own a token of a head, eight channels each, so that every
+// access is 16 bytes of numbers or the 4 to 16 bytes of their codes.
+#include "lm_cache.h"
+
+namespace qnn_lm {
+
+struct TokenArgs {
+    const void *k, *v;
+    int64_t ks[3], vs[3];  // elements: sequence, token, head
+    int32_t t;
+    uint32_t tokens;       // b * t * 2 * heads
+    const int32_t *lens, *counts;
+};
+
+// Index of this thread's token: (sequence, token, key or value, head), the
+// head fastest.
+struct Token {
+    int32_t seq, i, which, head;
+};
+__device__ __forceinline__ Token token_of(uint32_t n, int32_t heads, int32_t t)
+{
+    Token o;
+    o.head = n % heads;
+    n /= heads;
+    o.which = n & 1;
+    n >>= 1;
+    o.i = n % t;
+    o.seq = n / t;
+    return o;
+}
+
+template <class N, int BITS, int DIM>
+__global__ void __launch_bounds__(256) append_kernel(CacheArgs c, TokenArgs a)
+{
+    constexpr int LANES = DIM / 8;
+    const uint32_t n = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES;
+    if (n >= a.tokens)
+        return;
+    const Token o = token_of(n, c.heads, a.t);
+    if (a.counts && o.i >= a.counts[o.seq])
+        return;
+    const Slot s = find_slot(c, o.seq, (int64_t)a.lens[o.seq] + o.i);
+    if (s.page < 0)
+        return;
+    const int64_t *st = o.which ? a.vs : a.ks;
+    const typename N::T *src =
+        (const typename N::T *)(o.which ? a.v : a.k) + o.seq * st[0] + o.i * st[1] + o.head * st[2] + lane * 8;
+    uint8_t *dst = o.which ? c.v + s.page * c.v_page + o.head * c.v_head + s.slot * c.v_slot
+                           : c.k + s.page * c.k_page + o.head * c.k_head + s.slot * c.k_slot;
+    if constexpr (BITS == 16) {
+        *(u4 *)(dst + lane * 16) = *(const u4 *)src;
+    } else {
+        float v[8];
+        load8<N>(src, 0, v);
+        // the largest magnitude, by bits: infinity and NaN are above every finite number
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+#pragma unroll
+        for (int m = 1; m < LANES; m <<= 1)
+            top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
+        constexpr float most = BITS == 8 ? 127.f : 7.f;
+        const bool finite = top < 0x7F800000u;
+        const float scale = finite ? __uint_as_float(top) / most : __uint_as_float(0x7FC00000u);
+        uint32_t code[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q = finite && scale > 0.f ? rintf(v[e] / scale) : 0.f;
+            code[e] = (uint32_t)(int32_t)fminf(fmaxf(q, -most), most);
+        }
+        if constexpr (BITS == 8) {
+            u2 r;
+            r.x = (code[0] & 255) | (code[1] & 255) << 8 | (code[2] & 255) << 16 | code[3] << 24;
+            r.y = (code[4] & 255) | (code[5] & 255) << 8 | (code[6] & 255) << 16 | code[7] << 24;
+            *(u2 *)(dst + lane * 8) = r;
+        } else {
+            uint32_t r = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                r |= (code[e] & 15) << 4 * e;
+            *(uint32_t *)(dst + lane * 4) = r;
+        }
+        if (lane == 0)
+            (o.which ? c.v_scale : c.k_scale)[scale_at(c, s, o.head)] = scale;
+    }
+}
+
+struct ReadArgs {
+    void *k, *v;
+    int32_t t;
+    uint32_t tokens;          // b * t * 2 * heads
+    const int32_t *start;
+};
+
+// C: the number type of a 16-bit cache; N: of the result.
+template <class N, class C, int BITS, int DIM>
+__global__ void __launch_bounds__(256) read_kernel(CacheArgs c, ReadArgs a)
+{
+    constexpr int LANES = DIM / 8;
+    const uint32_t n = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES;
+    if (n >= a.tokens)
+        return;
+    const Token o = token_of(n, c.heads, a.t);
+    void *dst = o.which ? a.v : a.k;
+    if (!dst)
+        return;
+    const int64_t at = (((int64_t)o.seq * a.t + o.i) * c.heads + o.head) * DIM + lane * 8;
+    const Slot s = find_slot(c, o.seq, (int64_t)a.start[o.seq] + o.i);
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (s.page >= 0) {
+        const uint8_t *src = o.which ? c.v + s.page * c.v_page + o.head * c.v_head + s.slot * c.v_slot
+                                     : c.k + s.page * c.k_page + o.head * c.k_head + s.slot * c.k_slot;
+        if constexpr (BITS == 16) {
+            load8<C>(src, lane * 8, v);
+        } else {
+            const float scale = (o.which ? c.v_scale : c.k_scale)[scale_at(c, s, o.head)];
+            if constexpr (BITS == 8) {
+                const u2 r = *(const u2 *)(src + lane * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] = (float)(int8_t)(r[e / 4] >> 8 * (e % 4)) * scale;
+            } else {
+                const uint32_t r = *(const uint32_t *)(src + lane * 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] = (float)((int32_t)(r << (28 - 4 * e)) >> 28) * scale;
+            }
+        }
+    }
+    store8<N>(dst, at, v);
+}
+
+// A workgroup owns the keys or the values of one head of one sequence, and
+// moves as many tokens at a time as it has lanes for: all of them are read
+// before the first is written.  Entries ascend, so a later read never finds
+// what an earlier batch wrote.
+template <int ROW>  // bytes of a token
+__global__ void __launch_bounds__(256) keep_kernel(CacheArgs c, int32_t t, const int32_t *lens, const int32_t *path,
+                                                   const int32_t *kept)
+{
+    constexpr int LANES = ROW / 16, BATCH = 256 / LANES;
+    const int32_t seq = blockIdx.y, head = blockIdx.x >> 1, which = blockIdx.x & 1;
+    const int lane = threadIdx.x % LANES;
+    const int32_t count = min(kept[seq], t);
+    const int64_t len = lens[seq];
+    uint8_t *base = which ? c.v + head * c.v_head : c.k + head * c.k_head;
+    const int64_t sp = which ? c.v_page : c.k_page, ss = which ? c.v_slot : c.k_slot;
+    float *scale = which ? c.v_scale : c.k_scale;
+    for (int32_t j0 = 0; j0 < count; j0 += BATCH) {
+        const int32_t j = j0 + threadIdx.x / LANES;
+        Slot to = {-1, 0}, from = {-1, 0};
+        if (j < count) {
+            const int32_t p = path[(int64_t)seq * t + j];
+            if (p > j && p < t) {
+                from = find_slot(c, seq, len + p);
+                to = find_slot(c, seq, len + j);
+            }
+        }
+        const bool move = from.page >= 0 && to.page >= 0;
+        u4 r = {0, 0, 0, 0};
+        float sc = 0;
+        if (move) {
+            r = *(const u4 *)(base + from.page * sp + from.slot * ss + lane * 16);
+            if (scale && lane == 0)
+                sc = scale[scale_at(c, from, head)];
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // every read of the batch is back
+        __syncthreads();
+        if (move) {
+            *(u4 *)(base + to.page * sp + to.slot * ss + lane * 16) = r;
+            if (scale && lane == 0)
+                scale[scale_at(c, to, head)] = sc;
+        }
+    }
+}
+
+#define QNN_LM_DIMS(CALL) \
+    switch (dim) {        \
+    case 64: CALL(64)     \
+    case 128: CALL(128)   \
+    case 256: CALL(256)   \
+    default: return hipErrorInvalidValue; \
+    }                     \
+    return hipGetLastError();
+
+template <class N, int BITS>
+static hipError_t append_bits(const CacheArgs &c, int dim, const TokenArgs &a, hipStream_t s)
+{
+#define CALL(D)                                                                                              \
+    hipLaunchKernelGGL((append_kernel<N, BITS, D>), dim3((a.tokens + 2048 / D - 1) / (2048 / D)), dim3(256), 0, s, c, a); \
+    break;
+    QNN_LM_DIMS(CALL)
+#undef CALL
+}
+
+hipError_t launch_append(const CacheArgs &c, int bits, int dim, int type, const void *k, const void *v,
+                         const int64_t *k_stride, const int64_t *v_stride, int t, const int32_t *lens,
+                         const int32_t *counts, hipStream_t s)
+{
+    TokenArgs a;
+    a.k = k;
+    a.v = v;
+    for (int i = 0; i < 3; ++i) {
+        a.ks[i] = k_stride[i];
+        a.vs[i] = v_stride[i];
+    }
+    a.t = t;
+    a.tokens = (uint32_t)((int64_t)c.b * t * 2 * c.heads);
+    a.lens = lens;
+    a.counts = counts;
+    if (bits == 16)
+        return append_bits<Bf16, 16>(c, dim, a, s);  // 16-bit numbers are copied
+    if (type == QNN_LM_BF16)
+        return bits == 8 ? append_bits<Bf16, 8>(c, dim, a, s) : append_bits<Bf16, 4>(c, dim, a, s);
+    return bits == 8 ? append_bits<F16, 8>(c, dim, a, s) : append_bits<F16, 4>(c, dim, a, s);
+}
+
+template <class N, class C, int BITS>
+static hipError_t read_bits(const CacheArgs &c, int dim, const ReadArgs &a, hipStream_t s)
+{
+#define CALL(D)                                                                                              \
+    hipLaunchKernelGGL((read_kernel<N, C, BITS, D>), dim3((a.tokens + 2048 / D - 1) / (2048 / D)), dim3(256), 0, s, c, a); \
+    break;
+    QNN_LM_DIMS(CALL)
+#undef CALL
+}
+
+template <class N>
+static hipError_t read_typed(const CacheArgs &c, int bits, int dim, int cache_type, const ReadArgs &a, hipStream_t s)
+{
+    if (bits == 8)
+        return read_bits<N, Bf16, 8>(c, dim, a, s);
+    if (bits == 4)
+        return read_bits<N, Bf16, 4>(c, dim, a, s);
+    return cache_type == QNN_LM_BF16 ? read_bits<N, Bf16, 16>(c, dim, a, s) : read_bits<N, F16, 16>(c, dim, a, s);
+}
+
+hipError_t launch_read(const CacheArgs &c, int bits, int dim, int type, int cache_type, int t, const int32_t *start,
+                       void *k, void *v, hipStream_t s)
+{
+    ReadArgs a;
+    a.k = k;
+    a.v = v;
+    a.t = t;
+    a.tokens = (uint32_t)((int64_t)c.b * t * 2 * c.heads);
+    a.start = start;
+    if (type == QNN_LM_F32)
+        return read_typed<F32>(c, bits, dim, cache_type, a, s);
+    return type == QNN_LM_BF16 ? read_typed<Bf16>(c, bits, dim, cache_type, a, s)
+                               : read_typed<F16>(c, bits, dim, cache_type, a, s);
+}
+
+hipError_t launch_keep(const CacheArgs &c, int bits, int dim, int t, const int32_t *lens, const int32_t *path,
+                       const int32_t *kept, hipStream_t s)
+{
+    const dim3 grid(2 * c.heads, c.b);
+    switch (dim * bits / 8) {
+#define CASE(ROW)                                                                                   \
+    case ROW:                                                                                       \
+        hipLaunchKernelGGL(keep_kernel<ROW>, grid, dim3(256), 0, s, c, t, lens, path, kept);        \
+        break;
+        CASE(32) CASE(64) CASE(128) CASE(256) CASE(512)
+#undef CASE
+    default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace qnn_lm

@@ -1,0 +1,196 @@
+// The linear layer for few rows (a token, a tree of drafts): bound by reading
+// the weights once.
+//
+// y = x w^T on the 16x16x32 matrix instruction, A = 16 rows of x, B = 16 rows
+// of weights.  A lane holds NF eights of consecutive codes of one row of
+// weights, loaded straight from memory into registers (16 bytes where the
+// codes allow it) and expanded there: nothing is staged, nothing is shared, no
+// barrier in the loop.  The four lanes of a row take consecutive pieces, so a
+// step covers 32 NF columns of k in an order of its own; x is read at the same
+// columns.  A step lies inside one group, so a group's scale multiplies the
+// step's sums (exact products, fp32 sums), one scale a lane.
+// A workgroup owns 16 WR rows of weights (16 WR / 2 outputs where gated: gate
+// and up rows side by side) and 16 NC rows of x; its waves split k and are
+// joined through local memory in a fixed order.
+#pragma once
+
+#include "lm_matmul.h"
+
+namespace qnn_lm {
+
+template <class N, int BITS, int NF, int WR, int NC, bool GATED>
+struct RowsTile {
+    static constexpr int kStep = 32 * NF;
+    uint32_t w[WR][kRaw<BITS, NF> < 4 ? 1 : kRaw<BITS, NF> / 4];
+    typename N::V8 x[NC][NF];
+    float scale[WR];
+
+    __device__ __forceinline__ void load(const MatmulArgs &a, const uint8_t *const (&wp)[WR],
+                                         const typename N::T *const (&xp)[NC], const float *const (&sp)[WR],
+                                         int32_t k0, int kq)
+    {
+        const int32_t k = k0 + kq * 8 * NF;  // this lane's piece
+        const bool in = k < a.k;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                u4 v = {0, 0, 0, 0};
+                if (in && xp[c])
+                    v = *(const u4 *)(xp[c] + k + 8 * f);
+                x[c][f] = __builtin_bit_cast(typename N::V8, v);
+            }
+#pragma unroll
+        for (int r = 0; r < WR; ++r) {
+#pragma unroll
+            for (uint32_t &v : w[r])
+                v = 0;
+            if (in)
+                load_raw<kRaw<BITS, NF>>(wp[r] + (int64_t)k * BITS / 8, w[r]);
+            if constexpr (BITS != 16)
+                scale[r] = a.groups > 1 ? sp[r][k0 / a.group] : 1.f;
+        }
+    }
+
+    __device__ __forceinline__ void add(f4 (&acc)[WR][NC], bool grouped) const
+    {
+#pragma unroll
+        for (int r = 0; r < WR; ++r) {
+            f4 part[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                part[c] = grouped ? (f4){0, 0, 0, 0} : acc[r][c];
+            steps<0>(r, part);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                acc[r][c] = grouped ? acc[r][c] + scale[r] * part[c] : part[c];
+        }
+    }
+
+    template <int F>
+    __device__ __forceinline__ void steps(int r, f4 (&part)[NC]) const
+    {
+        if constexpr (F < NF) {
+            const typename N::V8 b = expand<N, BITS, F>(w[r]);
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                part[c] = mfma16(x[c][F], b, part[c]);
+            steps<F + 1>(r, part);
+        }
+    }
+};
+
+template <class N, int BITS, int NF, int WR, int NC, bool GATED, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
+{
+    using Tile = RowsTile<N, BITS, NF, WR, NC, GATED>;
+    extern __shared__ f4 part[];  // [wave][WR][NC][64]
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int OUT = GATED ? 8 * WR : 16 * WR;  // outputs of a workgroup
+    const int32_t j0 = blockIdx.x * OUT, r0 = blockIdx.y * 16 * NC;
+    const uint8_t *wp[WR];
+    const float *sp[WR];
+    const typename N::T *xp[NC];
+#pragma unroll
+    for (int r = 0; r < WR; ++r) {
+        // rows past the last one repeat it; their sums are not stored
+        const int32_t j = min(j0 + (GATED ? r / 2 : r) * 16 + l16, a.m - 1);
+        const int64_t row = GATED && (r & 1) ? a.m + j : j;
+        wp[r] = (const uint8_t *)a.w + row * a.w_row;
+        sp[r] = BITS == 16 ? nullptr : a.scale + row * a.groups;
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int32_t r = r0 + c * 16 + l16;
+        xp[c] = r < a.r ? (const typename N::T *)a.x + r * a.x_pitch : nullptr;
+    }
+    f4 acc[WR][NC];
+#pragma unroll
+    for (int r = 0; r < WR; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            acc[r][c] = (f4){0, 0, 0, 0};
+    // a wave's share of the steps, in one piece
+    const int32_t steps = (a.k + Tile::kStep - 1) / Tile::kStep;
+    const int32_t share = (steps + WAVES - 1) / WAVES;
+    const int32_t first = min(wave * share, steps), last = min(first + share, steps);
+    const bool grouped = BITS != 16 && a.groups > 1;
+    Tile cur, next;
+    if (first < last)
+        cur.load(a, wp, xp, sp, first * Tile::kStep, kq);
+    for (int32_t s = first; s < last; ++s) {
+        if (s + 1 < last)
+            next.load(a, wp, xp, sp, (s + 1) * Tile::kStep, kq);
+        cur.add(acc, grouped);
+        cur = next;
+    }
+#pragma unroll
+    for (int r = 0; r < WR; ++r) {
+        float unscale = kUnscale<BITS>;
+        if (BITS != 16 && a.groups == 1)
+            unscale *= sp[r][0];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            part[((wave * WR + r) * NC + c) * 64 + lane] = acc[r][c] * unscale;
+    }
+    __syncthreads();
+    // element e of the workgroup's outputs: lane l of a tile holds column
+    // l % 16 at rows 4 * (l / 16) .. + 3
+    constexpr int OT = GATED ? WR / 2 : WR;
+    for (int e = threadIdx.x; e < OT * NC * 64; e += 64 * WAVES) {
+        const int l = e & 63, c = (e >> 6) % NC, o = (e >> 6) / NC;
+        f4 t = {0, 0, 0, 0}, up = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            t += part[((w * WR + (GATED ? 2 * o : o)) * NC + c) * 64 + l];
+            if constexpr (GATED)
+                up += part[((w * WR + 2 * o + 1) * NC + c) * 64 + l];
+        }
+        const int32_t col = j0 + o * 16 + (l & 15);
+        if (col >= a.m)
+            continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t row = r0 + c * 16 + 4 * (l >> 4) + i;
+            if (row < a.r)
+                finish<N>(a, row, col, t[i], up[i]);
+        }
+    }
+}
+
+template <class N, int BITS, int NF, int WR, int NC, bool GATED, int WAVES>
+hipError_t launch_rows(const MatmulArgs &a, hipStream_t s)
+{
+    constexpr int OUT = GATED ? 8 * WR : 16 * WR;
+    const dim3 grid((a.m + OUT - 1) / OUT, (a.r + 16 * NC - 1) / (16 * NC));
+    hipLaunchKernelGGL((matmul_rows_kernel<N, BITS, NF, WR, NC, GATED, WAVES>), grid, dim3(64 * WAVES),
+                       WAVES * WR * NC * 64 * sizeof(f4), s, a);
+    return hipGetLastError();
+}
+
+template <class N, int BITS, int NF>
+hipError_t launch_rows_sized(const MatmulArgs &a, hipStream_t s)
+{
+    if (a.gated)
+        return a.r <= 16 ? launch_rows<N, BITS, NF, 2, 1, true, 8>(a, s) : launch_rows<N, BITS, NF, 2, 4, true, 8>(a, s);
+    return a.r <= 16 ? launch_rows<N, BITS, NF, 1, 1, false, 8>(a, s) : launch_rows<N, BITS, NF, 2, 4, false, 8>(a, s);
+}
+
+// A lane's piece is a quarter of a group at most.
+template <class N, int BITS>
+hipError_t launch_rows_bits(const MatmulArgs &a, hipStream_t s)
+{
+    if constexpr (BITS == 16)
+        return launch_rows_sized<N, 16, 1>(a, s);
+    const int32_t g = a.groups > 1 ? a.group : 128;
+    if (g == 32)
+        return launch_rows_sized<N, BITS, 1>(a, s);
+    if (g == 64 || BITS == 8)
+        return launch_rows_sized<N, BITS, 2>(a, s);
+    if constexpr (BITS < 8)
+        return launch_rows_sized<N, BITS, 4>(a, s);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace qnn_lm
