@@ -1,0 +1,6 @@
+// The linear layer's kernels for bf16 and 16-bit weights.
+#include "lm_matmul_impl.h"
+
+namespace qnn_lm {
+hipError_t launch_matmul_bf16_w16(const MatmulArgs &a, hipStream_t s) { return launch_matmul_one<Bf16, 16>(a, s); }
+}  // namespace qnn_lm

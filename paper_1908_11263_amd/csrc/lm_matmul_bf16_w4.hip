@@ -1,0 +1,6 @@
+// The linear layer's kernels for bf16 and 4-bit weights.
+#include "lm_matmul_impl.h"
+
+namespace qnn_lm {
+hipError_t launch_matmul_bf16_w4(const MatmulArgs &a, hipStream_t s) { return launch_matmul_one<Bf16, 4>(a, s); }
+}  // namespace qnn_lm

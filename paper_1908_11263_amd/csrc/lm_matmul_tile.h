@@ -1,0 +1,399 @@
+// The linear layer for many rows (prompts, large batches of trees): bound by
+// the matrix cores.
+//
+// y = x w^T on the 32x32x16 matrix instruction, A = 32 rows of x, B = 32 rows
+// of weights.  A workgroup of four waves owns 32 TF rows of x and 128 WF rows of
+// weights; a wave all of the former and 32 WF of the latter, so that every code
+// is expanded once a workgroup, in registers, by the wave that multiplies it.
+// x and the packed codes stream through local memory in steps of KS columns,
+// copied there by the memory unit itself (no registers), STAGES - 1 steps
+// ahead, with one barrier a step.  Sixteen-byte pieces are permuted within a
+// row by the row's number, so that the fragments' reads spread over the banks;
+// the copy writes them in lane order, so the permutation is applied to the
+// address that a lane reads from memory.
+//
+// k is taken in blocks of 32: lane l holds row l % 32 at k = 16 (l / 32) .. +
+// 15 of the block, two eights, the same for x and weights.
+//
+// Group scales: the sums are kept in units of the current group's scale and
+// multiplied by the ratio of the old scale to the new one where a group ends
+// (one fp32 product, where a second set of accumulators would not fit); scales
+// of zero, whose ratio is not finite, keep the unit and clear the group's codes.
+#pragma once
+
+#include "lm_matmul.h"
+#include "qnn_internal.h"
+
+namespace qnn_lm {
+
+__device__ __forceinline__ f16v mfma32(bf8 a, bf8 b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f16v mfma32(h8 a, h8 b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// Copies 16 (or 4) bytes a lane from base + off to local memory at lds + 16 (4)
+// * lane, without registers.  The counter of outstanding loads is waited for
+// by hand (wait_copies).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is reserved; the compiler keeps nothing there)
+template <int BYTES>
+__device__ __forceinline__ void copy_to_lds(const void *base, uint32_t off, uint32_t lds)
+{
+    // (a wait state between the write of m0 and the copy that uses it)
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
+                     : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base)
+                     : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// Until at most N of this wave's copies are outstanding and its reads of local
+// memory are back.
+template <int N>
+__device__ __forceinline__ void wait_copies()
+{
+    static_assert(N < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+template <int BITS, int TF, int WF, int GPB>  // GPB: groups of a step (0: one scale a row)
+struct TileShape {
+    static constexpr int KS = BITS == 16 ? 32 : 64;    // columns of a step
+    static constexpr int BM = 32 * TF, BN = 128 * WF;  // rows of x and of weights
+    static constexpr int kXRow = KS * 2, kWRow = KS * BITS / 8;  // bytes of a staged row
+    static constexpr int kXChunks = kXRow / 16;
+    static constexpr int kWUnit = BITS >= 4 ? 16 : 4;  // bytes of a copy of weights
+    static constexpr int kWUnits = kWRow / kWUnit;     // of a row
+    static constexpr int kXCopies = BM * kXRow / 1024 / 4;         // instructions of a wave a step
+    static constexpr int kWCopies = BN * kWUnits / 64 / 4;
+    static constexpr int kCopies = kXCopies + kWCopies + GPB;
+    static constexpr int kXBytes = BM * kXRow, kWBytes = BN * kWRow;
+    static constexpr int kStage = kXBytes + kWBytes + GPB * BN * 4;
+    // two workgroups a compute unit
+    static constexpr int kStages = 3 * kStage <= 80 * 1024 ? 3 : 2;
+    static constexpr int kOutPitch = BN + 4;                  // floats
+    static constexpr int kOut = 32 * kOutPitch * 4;
+    static constexpr int kLds = kStages * kStage > kOut ? kStages * kStage : kOut;
+
+    // place of piece c of row r among the row's pieces
+    static __device__ __forceinline__ int x_place(int r, int c)
+    {
+        return c ^ (kXChunks == 8 ? r & 7 : (r >> 1) & 3);
+    }
+    static __device__ __forceinline__ int w_place(int r, int c)
+    {
+        if constexpr (BITS == 8 || BITS == 16)  // four pieces
+            return c ^ ((r >> 1) & 3);
+        else if constexpr (BITS == 4)
+            return c ^ ((r >> 2) & 1);
+        else
+            return c;
+    }
+};
+
+struct TileGrid {
+    int32_t tm, tn;  // tiles of rows of x, of rows of weights
+};
+
+// The products of eight F of a block.
+template <class N, int BITS, int TF, int WF, int GPB, int F>
+__device__ __forceinline__ void eights(const uint8_t *xs, const uint32_t (&raw)[WF][BITS >= 2 ? BITS / 2 : 1],
+                                       const uint32_t (&clear)[WF], f16v (&acc)[TF][WF], int b, int l32, int half)
+{
+    using S = TileShape<BITS, TF, WF, GPB>;
+    typename N::V8 x[TF], w[WF];
+#pragma unroll
+    for (int m = 0; m < TF; ++m) {
+        const int r = m * 32 + l32;
+        x[m] = *(const typename N::V8 *)(xs + r * S::kXRow + S::x_place(r, 4 * b + 2 * half + F) * 16);
+    }
+#pragma unroll
+    for (int n = 0; n < WF; ++n) {
+        w[n] = expand<N, BITS, F>(raw[n]);
+        if constexpr (GPB && BITS == 1) {
+            u4 v = __builtin_bit_cast(u4, w[n]);
+            v &= ~clear[n];
+            w[n] = __builtin_bit_cast(typename N::V8, v);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < WF; ++n)
+#pragma unroll
+        for (int m = 0; m < TF; ++m)
+            acc[m][n] = mfma32(x[m], w[n], acc[m][n]);
+}
+
+template <class N, int BITS, int TF, int WF, int GPB, bool GATED>
+__global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileGrid g)
+{
+    using S = TileShape<BITS, TF, WF, GPB>;
+    static_assert(!GATED || WF == 2, "a wave holds a gate's rows and their partners");
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int OUT = GATED ? S::BN / 2 : S::BN;  // outputs of a row
+
+    // Tiles in an order that keeps an XCD (workgroups go round the eight of
+    // them) on neighbouring tiles, eight tiles of x to a column of weights.
+    const int32_t tiles = g.tm * g.tn;
+    int32_t t = blockIdx.x;
+    {
+        const int32_t q = tiles >> 3, rem = tiles & 7, x = t & 7;
+        t = x * q + min(x, rem) + (t >> 3);
+    }
+    const int32_t band = t / (8 * g.tn), first = band * 8, high = min(8, g.tm - first);
+    const int32_t in = t - band * 8 * g.tn;
+    const int32_t r0 = (first + in % high) * S::BM, j0 = in / high * OUT;
+
+    // What this lane copies: offsets from the tile's first row of x, and from
+    // the first row of weights of each copy (all of a copy's rows lie in one of
+    // the two halves of a gated layer).
+    const uint8_t *xb = (const uint8_t *)a.x + (int64_t)r0 * a.x_pitch * 2;
+    uint32_t xo[S::kXCopies], wo[S::kWCopies];
+    int xc[S::kXCopies], wc[S::kWCopies];  // the piece, for the last step
+#pragma unroll
+    for (int i = 0; i < S::kXCopies; ++i) {
+        const int e = (wave * S::kXCopies + i) * 64 + lane, r = e / S::kXChunks;
+        xc[i] = S::x_place(r, e % S::kXChunks);
+        xo[i] = (uint32_t)min(r, a.r - 1 - r0) * (uint32_t)(a.x_pitch * 2) + xc[i] * 16;
+    }
+    const uint8_t *wb[S::kWCopies];
+#pragma unroll
+    for (int i = 0; i < S::kWCopies; ++i) {
+        const int e0 = (wave * S::kWCopies + i) * 64, e = e0 + lane, r = e / S::kWUnits;
+        wc[i] = S::w_place(r, e % S::kWUnits);
+        if constexpr (GATED) {
+            // staged row 64 w + 32 f + r is row 32 w + r of half f
+            const int j = j0 + (r >> 6) * 32 + (r & 31);
+            const int up = (e0 / S::kWUnits >> 5) & 1;
+            wb[i] = (const uint8_t *)a.w + (int64_t)up * a.m * a.w_row + (int64_t)j0 * a.w_row;
+            wo[i] = (uint32_t)(min(j, a.m - 1) - j0) * (uint32_t)a.w_row + wc[i] * S::kWUnit;
+        } else {
+            wb[i] = (const uint8_t *)a.w + (int64_t)j0 * a.w_row;
+            wo[i] = (uint32_t)(min(j0 + r, a.m - 1) - j0) * (uint32_t)a.w_row + wc[i] * S::kWUnit;
+        }
+    }
+    // scales: one a lane and group (of half wave / 2 where gated)
+    const float *sb = nullptr;
+    uint32_t so = 0;
+    if constexpr (GPB) {
+        const int e = (WF == 2 ? wave : wave & 1) * 64 + lane;
+        const int up = GATED ? wave >> 1 : 0, j = GATED ? j0 + (e & 127) : j0 + e;
+        sb = a.scale + ((int64_t)up * a.m + j0) * a.groups;
+        so = (uint32_t)(min(j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+
+    auto issue = [&](int32_t step, int buf) {
+        const int32_t k0 = step * S::KS, left = a.k - k0;  // a multiple of 32
+        const uint32_t at = lds0 + buf * S::kStage;
+        const uint8_t *x = xb + (int64_t)k0 * 2;
+        const bool whole = left >= S::KS;
+#pragma unroll
+        for (int i = 0; i < S::kXCopies; ++i)
+            // (pieces past the row's end, never read, copy its first again)
+            copy_to_lds<16>(x, whole || xc[i] * 8 < left ? xo[i] : xo[i] - xc[i] * 16,
+                            at + (wave * S::kXCopies + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < S::kWCopies; ++i)
+            copy_to_lds<S::kWUnit>(wb[i] + (int64_t)k0 * BITS / 8,
+                                   whole || wc[i] * (S::kWUnit * 8 / BITS) < left ? wo[i] : wo[i] - wc[i] * S::kWUnit,
+                                   at + S::kXBytes + (wave * S::kWCopies + i) * 64 * S::kWUnit);
+        if constexpr (GPB) {
+            const int32_t grp = k0 >> __builtin_ctz(a.group);
+#pragma unroll
+            for (int i = 0; i < GPB; ++i)
+                copy_to_lds<4>(sb + min(grp + i, a.groups - 1), so,
+                               at + S::kXBytes + S::kWBytes + (i * S::BN + (WF == 2 ? wave : wave & 1) * 64) * 4);
+        }
+    };
+
+    f16v acc[TF][WF];
+#pragma unroll
+    for (int m = 0; m < TF; ++m)
+#pragma unroll
+        for (int n = 0; n < WF; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                acc[m][n][i] = 0.f;
+    float unit[WF];
+    uint32_t clear[WF];  // 0 where the group's codes count
+#pragma unroll
+    for (int n = 0; n < WF; ++n)
+        unit[n] = 1.f, clear[n] = 0;
+
+    const int32_t steps = (a.k + S::KS - 1) / S::KS;
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s)
+        issue(min(s, steps - 1), s);
+    int buf = 0;
+    for (int32_t s = 0; s < steps; ++s) {
+        wait_copies<(S::kStages - 2) * S::kCopies>();
+        __builtin_amdgcn_s_barrier();
+        {
+            // (past the last step it is copied again, so that the counts stay)
+            const int to = buf == 0 ? S::kStages - 1 : buf - 1;
+            issue(min(s + S::kStages - 1, steps - 1), to);
+        }
+        const uint8_t *xs = lds + buf * S::kStage, *ws = xs + S::kXBytes;
+        const float *ss = (const float *)(ws + S::kWBytes);
+        const int blocks = min(a.k - s * S::KS, S::KS) >> 5;
+#pragma unroll
+        for (int b = 0; b < S::KS / 32; ++b) {
+            if (b >= blocks)
+                break;
+            if constexpr (GPB) {
+                const int32_t k = s * S::KS + b * 32;
+                if ((k & (a.group - 1)) == 0) {
+#pragma unroll
+                    for (int n = 0; n < WF; ++n) {
+                        const float sc = ss[(GPB == 2 ? b * S::BN : 0) + (GATED ? n * 128 + wave * 32 : wave * 32 * WF + n * 32) + l32];
+                        const float ratio = k == 0 ? 0.f : unit[n] / sc;
+                        const bool zero = sc == 0.f || __builtin_isinf(ratio);
+                        clear[n] = zero ? 0xFFFFFFFFu : 0;
+                        const float f = zero ? 1.f : ratio;
+                        unit[n] = zero ? unit[n] : sc;
+                        if (k != 0)
+#pragma unroll
+                            for (int m = 0; m < TF; ++m)
+                                acc[m][n] *= f;
+                    }
+                }
+            }
+            uint32_t raw[WF][BITS >= 2 ? BITS / 2 : 1];
+#pragma unroll
+            for (int n = 0; n < WF; ++n) {
+                const int r = (wave * WF + n) * 32 + l32;
+                const uint8_t *p = ws + r * S::kWRow;
+                if constexpr (BITS == 16) {
+#pragma unroll
+                    for (int f = 0; f < 2; ++f)
+                        load_words<4>(p + S::w_place(r, 2 * half + f) * 16, raw[n] + 4 * f);
+                } else if constexpr (BITS == 8) {
+                    load_words<4>(p + S::w_place(r, 2 * b + half) * 16, raw[n]);
+                } else if constexpr (BITS == 4) {
+                    load_words<2>(p + S::w_place(r, b) * 16 + half * 8, raw[n]);
+                } else {
+                    load_raw<2 * BITS>(p + b * 4 * BITS + half * 2 * BITS, raw[n]);
+                }
+            }
+            // (a 1-bit code has no zero: its numbers are cleared instead)
+            if constexpr (GPB && BITS != 1)
+#pragma unroll
+                for (int n = 0; n < WF; ++n)
+#pragma unroll
+                    for (uint32_t &w : raw[n])
+                        w &= ~clear[n];
+            eights<N, BITS, TF, WF, GPB, 0>(xs, raw, clear, acc, b, l32, half);
+            eights<N, BITS, TF, WF, GPB, 1>(xs, raw, clear, acc, b, l32, half);
+        }
+        buf = buf == S::kStages - 1 ? 0 : buf + 1;
+    }
+    // the copies of the last steps, made again, are there before local memory
+    // is used anew
+    wait_copies<0>();
+    __syncthreads();
+
+    // Epilogue: sums to results in registers, 32 rows at a time through local
+    // memory, from where rows are written (and the residual read) 16 bytes a lane.
+    float *out = (float *)lds;
+    float bias[WF];
+#pragma unroll
+    for (int n = 0; n < WF; ++n) {
+        const int32_t j = min(j0 + (GATED ? wave * 32 : (wave * WF + n) * 32) + l32, a.m - 1);
+        const int64_t row = GATED && n ? (int64_t)a.m + j : j;
+        unit[n] *= kUnscale<BITS>;
+        if (BITS != 16 && !GPB)
+            unit[n] *= a.scale[row];
+        bias[n] = a.bias ? a.bias[row] : 0.f;
+    }
+    const bool wide = ((a.m | (int32_t)a.y_pitch | (a.residual ? (int32_t)a.residual_pitch : 0)) & 7) == 0;
+#pragma unroll
+    for (int m = 0; m < TF; ++m) {
+        if (r0 + m * 32 >= a.r)
+            break;
+        if (m)
+            __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float *p = out + (8 * (i / 4) + 4 * half + i % 4) * S::kOutPitch + l32;
+            if constexpr (GATED) {
+                p[wave * 32] = activate(acc[m][0][i] * unit[0] + bias[0], a.act) * (acc[m][1][i] * unit[1] + bias[1]);
+            } else {
+#pragma unroll
+                for (int n = 0; n < WF; ++n)
+                    p[(wave * WF + n) * 32] = activate(acc[m][n][i] * unit[n] + bias[n], a.act);
+            }
+        }
+        __syncthreads();
+        constexpr int LANES = OUT / 8;  // of a row
+#pragma unroll 1
+        for (int r = threadIdx.x / LANES; r < 32; r += 256 / LANES) {
+            const int64_t row = r0 + m * 32 + r;
+            const int32_t col = j0 + threadIdx.x % LANES * 8;
+            if (row >= a.r || col >= a.m)
+                continue;
+            float v[8], res[8];
+            load8<F32>(out, r * S::kOutPitch + threadIdx.x % LANES * 8, v);
+            if (wide) {
+                if (a.residual) {
+                    load8<N>(a.residual, row * a.residual_pitch + col, res);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[e] += res[e];
+                }
+                store8<N>(a.y, row * a.y_pitch + col, v);
+            } else {
+                for (int e = 0; e < 8 && col + e < a.m; ++e) {
+                    if (a.residual)
+                        v[e] += load1<N>(a.residual, row * a.residual_pitch + col + e);
+                    store1<N>(a.y, row * a.y_pitch + col + e, v[e]);
+                }
+            }
+        }
+    }
+}
+
+template <class N, int BITS, int TF, int WF, int GPB, bool GATED>
+hipError_t launch_tile(const MatmulArgs &a, hipStream_t s)
+{
+    using S = TileShape<BITS, TF, WF, GPB>;
+    constexpr int OUT = GATED ? S::BN / 2 : S::BN;
+    TileGrid g;
+    g.tm = (a.r + S::BM - 1) / S::BM;
+    g.tn = (a.m + OUT - 1) / OUT;
+    const void *kernel = (const void *)matmul_tile_kernel<N, BITS, TF, WF, GPB, GATED>;
+    if constexpr (S::kLds > 64 * 1024) {
+        static std::atomic<uint64_t> devices{0};
+        qnn::allow_large_lds(kernel, devices);
+    }
+    hipLaunchKernelGGL((matmul_tile_kernel<N, BITS, TF, WF, GPB, GATED>), dim3((unsigned)g.tm * g.tn), dim3(256), S::kLds,
+                       s, a, g);
+    return hipGetLastError();
+}
+
+template <class N, int BITS, int GPB>
+hipError_t launch_tile_groups(const MatmulArgs &a, hipStream_t s)
+{
+    if (a.gated)
+        return launch_tile<N, BITS, 4, 2, GPB, true>(a, s);
+    return launch_tile<N, BITS, 4, 2, GPB, false>(a, s);
+}
+
+template <class N, int BITS>
+hipError_t launch_tile_bits(const MatmulArgs &a, hipStream_t s)
+{
+    if constexpr (BITS != 16) {
+        if (a.groups > 1)
+            return a.group == 32 ? launch_tile_groups<N, BITS, 2>(a, s) : launch_tile_groups<N, BITS, 1>(a, s);
+    }
+    return launch_tile_groups<N, BITS, 0>(a, s);
+}
+
+}  // namespace qnn_lm

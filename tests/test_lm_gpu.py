@@ -579,3 +579,19 @@ def test_graph_replays(lm):
         want = pass_through(lm, new)
         for x, y in zip(out, want):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2, 1])
+@pytest.mark.parametrize("r", [2, 50, 140])
+def test_matmul_zero_and_uneven_scales(lm, bits, r):
+    """Groups whose scale is zero, first, last and in a row, and groups of very different scales."""
+    g = gen(bits)
+    for group in (32, 64, 128):
+        L = layer(g, r, 1280, 150, bits, group, BF)
+        s = L["scale"]
+        s *= 10.0 ** torch.randint(-6, 7, s.shape, generator=g, device="cuda")
+        s[torch.rand(s.shape, generator=g, device="cuda") < 0.3] = 0
+        s[3], s[4, :-1], s[5, 1:] = 0, 0, 0
+        s[6, 1] = -s[6, 1]
+        s[7, 0] = 1e-42  # no normal number
+        check_matmul(lm, L, bits)
