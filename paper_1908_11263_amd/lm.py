@@ -16,7 +16,6 @@ will do whose last is 1 and whose others are multiples of 16 bytes: a view of
 """
 import collections
 import ctypes
-import math
 import os
 import struct
 
@@ -29,6 +28,8 @@ HEADER = os.path.join(os.path.dirname(qnn.HEADER), "qnn_lm.h")
 
 BF16, F16, F32 = 0, 1, 2
 _TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+_TYPES16 = {torch.bfloat16: BF16, torch.float16: F16}
+_U8, _I32, _F32 = torch.uint8, torch.int32, torch.float32
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 _NORMS = {"rms": 0, "layer": 1}
 
@@ -68,60 +69,75 @@ def _fn(name):
     return _f.get(name) or _load()[name]
 
 
-def _check(status, name):
-    if status != 0:
-        raise QnnError(status, name)
-
-
 def _bad(what):
     raise ValueError(what)
 
 
-def _on_device(*tensors):
-    """All given tensors live on the current device."""
-    device = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            _bad("tensors must be on the current device (cuda:%d): got one on %s" % (device, t.device))
+# A call of a small layer takes a few microseconds on the device: what follows
+# is written for the host's time (no helper call per tensor where one line
+# does, one read of an attribute that costs 0.1 us).
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda d: torch.cuda.current_stream(d).cuda_stream)
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _stream(d, stream):
+    """The stream's handle; d: the device of the call's tensors, which must be the current one."""
+    if d < 0:
+        if torch.cuda.is_available():
+            _bad("tensors must be on the current device")
+        return None  # (no device at all: the library says so)
+    if d != _current():
+        _bad("tensors must be on the current device (cuda:%d): got some on cuda:%d" % (_current(), d))
+    return _raw_stream(d) if stream is None else stream.cuda_stream
+
+
+def _elsewhere(t):
+    _bad("all tensors must be on one device: got one on %s" % t.device)
 
 
 def _alloc(shape, dtype, like, stream):
     """Uninitialised memory of the stream that will use it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _vector(t, n, what):
-    """A contiguous float32 vector of n, or None."""
-    if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
+def _alloc_like(t, stream):
+    """The same for a tensor like the contiguous t."""
+    if stream is None:
+        return torch.empty_like(t)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
+
+
+def _vector(t, n, d, what):
+    """The address of a contiguous float32 vector of n."""
+    if t.dtype is not _F32 or t.numel() != n or not t.is_contiguous():
         _bad("%s must be contiguous float32 of %d elements" % (what, n))
-    return t
+    if t.get_device() != d:
+        _elsewhere(t)
+    return t.data_ptr()
 
 
-def _ints(t, shape, what):
-    if t is not None and (t.dtype is not torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
-        _bad("%s must be contiguous int32 of shape %s" % (what, shape))
-    return t
+def _ints(t, n, d, what):
+    """The address of a contiguous int32 vector of n."""
+    if t.dtype is not _I32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        _bad("%s must be contiguous int32 of %d" % (what, n))
+    if t.get_device() != d:
+        _elsewhere(t)
+    return t.data_ptr()
 
 
-def _rows(t, what):
-    """(rows, channels, pitch) of a matrix, or of a stack of them that is one."""
-    if t.dim() < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        _bad("%s must be contiguous along its last axis" % what)
-    n = t.shape[-1]
-    if t.dim() == 1:
-        return 1, n, n
-    if t.dim() == 2:
-        return t.shape[0], n, t.stride(0) if t.shape[0] > 1 else n
-    if not t.is_contiguous():
-        _bad("%s: more than two axes must be contiguous" % what)
-    return t.numel() // n if n else 0, n, n
+def _pitch(t, n, what):
+    """Elements from one row of n to the next of a matrix, or of a stack of them that is one."""
+    if t.is_contiguous():
+        return n
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and n > 1):
+        _bad("%s must be contiguous along its last axis, and altogether with more than two axes" % what)
+    return st[0] if t.shape[0] > 1 else n
 
 
 def matmul(x, w, bits, scale=None, bias=None, act="none", gated=False, residual=None, out=None, stream=None):
@@ -134,49 +150,75 @@ def matmul(x, w, bits, scale=None, bias=None, act="none", gated=False, residual=
     float32 [rows] or [rows, groups], k / groups being 32, 64 or 128.  bias:
     float32 [rows].  Returns [..., m] of x's type; out may be residual."""
     dtype = x.dtype
-    kind = _TYPES.get(dtype, F32)
-    if kind == F32:
-        _bad("x must be bfloat16 or float16")
-    r, k, pitch = _rows(x, "x")
-    if r == 1 or pitch < k:
-        pitch = k if k % 8 == 0 else k + -k % 8
-    if w.dim() != 2 or not w.is_contiguous() or w.dtype is not (dtype if bits == 16 else torch.uint8):
-        _bad("w must be a contiguous matrix of uint8 (or, at 16 bits, of x's type)")
-    rows = w.shape[0]
-    if w.shape[1] * (1 if bits == 16 else 8) != k * (1 if bits == 16 else bits):
-        _bad("w has rows of %d for %d channels of %s bits" % (w.shape[1], k, bits))
-    if gated and rows % 2:
-        _bad("a gated layer has an even number of rows")
-    m = rows // 2 if gated else rows
+    kind = _TYPES16.get(dtype)
+    if kind is None or not x.dim():
+        _bad("x must be [..., k] bfloat16 or float16")
+    shape = x.shape
+    k = shape[-1]
+    lead = shape[:-1]
+    r = lead.numel()
+    pitch = k if x.is_contiguous() else _pitch(x, k, "x")
+    d = x.get_device()
+    if bits == 16:
+        if w.dtype is not dtype:
+            _bad("w must be of x's type at 16 bits")
+    elif w.dtype is not _U8:
+        _bad("w must be uint8 packed codes")
+    wshape = w.shape
+    if len(wshape) != 2 or not w.is_contiguous() or wshape[1] * (16 if bits == 16 else 8) != k * bits:
+        _bad("w must be contiguous rows of %d channels of %s bits: got %s" % (k, bits, tuple(wshape)))
+    if w.get_device() != d:
+        _elsewhere(w)
+    rows = wshape[0]
+    m = rows
+    if gated:
+        if rows % 2:
+            _bad("a gated layer has an even number of rows")
+        m = rows // 2
     group = 0
+    sp = bp = rp = None
     if scale is not None:
-        if scale.dtype is not torch.float32 or not scale.is_contiguous() or scale.shape[0] != rows or scale.dim() > 2:
+        st = scale.shape
+        if scale.dtype is not _F32 or not 1 <= len(st) <= 2 or st[0] != rows or not scale.is_contiguous():
             _bad("scale must be contiguous float32 [rows] or [rows, groups]")
-        if scale.dim() == 2 and scale.shape[1] != 1:
-            groups = scale.shape[1]
-            if groups == 0 or k % groups:
-                _bad("scale has %d groups for %d channels" % (groups, k))
-            group = k // groups
-    _vector(bias, rows, "bias")
-    shape = x.shape[:-1] + (m,)
-    rpitch = m
+        if len(st) == 2 and st[1] != 1:
+            if st[1] == 0 or k % st[1]:
+                _bad("scale has %d groups for %d channels" % (st[1], k))
+            group = k // st[1]
+        if scale.get_device() != d:
+            _elsewhere(scale)
+        sp = scale.data_ptr()
+    if bias is not None:
+        bp = _vector(bias, rows, d, "bias")
+    shape = lead + (m,)
+    rpitch = ypitch = m
     if residual is not None:
         if residual.dtype is not dtype or residual.shape != shape:
             _bad("residual must be of x's type and the result's shape")
-        rr, _, rpitch = _rows(residual, "residual")
+        if residual.get_device() != d:
+            _elsewhere(residual)
+        rpitch = _pitch(residual, m, "residual")
+        rp = residual.data_ptr()
+    handle = _stream(d, stream)
     if out is None:
-        out = _alloc(shape, dtype, x, stream)
-        ypitch = m
+        if stream is not None:
+            out = _alloc(shape, dtype, x, stream)
+        else:
+            out = x.new_empty(shape)
     else:
         if out.dtype is not dtype or out.shape != shape:
             _bad("out must be of x's type and shape %s" % (tuple(shape),))
-        _, _, ypitch = _rows(out, "out")
-    _on_device(x, w, scale, bias, residual, out)
+        if out.get_device() != d:
+            _elsewhere(out)
+        ypitch = _pitch(out, m, "out")
     s = _pack_linear(kind, bits, r, k, m, group, _ACTS[act], 1 if gated else 0, pitch, rpitch, ypitch)
-    size = _fn("qnn_lm_matmul_workspace")(s)
-    ws = _alloc((size,), torch.uint8, x, stream) if size else None
-    _check(_f["qnn_lm_matmul"](s, x.data_ptr(), w.data_ptr(), _ptr(scale), _ptr(bias), _ptr(residual), out.data_ptr(),
-                               _ptr(ws), size, qnn._stream_int(stream)), "qnn_lm_matmul")
+    f = _f or _load()
+    size = f["qnn_lm_matmul_workspace"](s)
+    ws = _alloc((size,), _U8, x, stream) if size else None
+    status = f["qnn_lm_matmul"](s, x.data_ptr(), w.data_ptr(), sp, bp, rp, out.data_ptr(),
+                                None if ws is None else ws.data_ptr(), size, handle)
+    if status:
+        raise QnnError(status, "qnn_lm_matmul")
     return out
 
 
@@ -192,42 +234,61 @@ def norm_residual(h, y=None, norm="rms", post=True, post_weight=None, post_bias=
     without a norm.  Weights and biases: float32 [d] or None.  gate: [d] or
     [gates, d] of y's type, each row for as many consecutive rows of y.  h_out
     may be h, out may be y."""
-    r, d, hpitch = _rows(h, "h")
-    ytype = (dtype or h.dtype) if y is None else y.dtype
-    kind, hkind = _TYPES.get(ytype), _TYPES.get(h.dtype)
-    if kind is None or hkind is None:
-        _bad("h and y must be bfloat16, float16 or float32")
-    if r == 1:
-        hpitch = d
+    hdtype = h.dtype
+    ytype = (dtype or hdtype) if y is None else y.dtype
+    kind, hkind = _TYPES.get(ytype), _TYPES.get(hdtype)
+    if kind is None or hkind is None or not h.dim():
+        _bad("h and y must be [..., d] bfloat16, float16 or float32")
+    shape = h.shape
+    d = shape[-1]
+    r = shape[:-1].numel()
+    hpitch = d if h.is_contiguous() else _pitch(h, d, "h")
+    dev = h.get_device()
+    handle = _stream(dev, stream)
     ypitch, gates = d, 0
+    yp = gp = hop = a = b = c = e = None
     if y is not None:
-        if y.shape != h.shape:
+        if y.shape != shape:
             _bad("h and y must have one shape")
-        _, _, ypitch = _rows(y, "y")
-        if r == 1:
-            ypitch = d
+        if y.get_device() != dev:
+            _elsewhere(y)
+        ypitch = d if y.is_contiguous() else _pitch(y, d, "y")
+        yp = y.data_ptr()
         if gate is not None:
-            if gate.dtype is not ytype or gate.shape[-1] != d or gate.dim() > 2 or not gate.is_contiguous():
+            if gate.dtype is not ytype or gate.dim() > 2 or gate.shape[-1:] != shape[-1:] or not gate.is_contiguous():
                 _bad("gate must be contiguous [d] or [gates, d] of y's type")
+            if gate.get_device() != dev:
+                _elsewhere(gate)
             gates = gate.numel() // d if d else 0
+            gp = gate.data_ptr()
         if h_out is None:
-            h_out = _alloc(h.shape, h.dtype, h, stream)
-        elif h_out.shape != h.shape or h_out.dtype is not h.dtype or not h_out.is_contiguous():
+            h_out = _alloc_like(h, stream) if hpitch == d else _alloc(shape, hdtype, h, stream)
+        elif h_out.shape != shape or h_out.dtype is not hdtype or not h_out.is_contiguous():
             _bad("h_out must be contiguous and like h")
+        elif h_out.get_device() != dev:
+            _elsewhere(h_out)
+        hop = h_out.data_ptr()
+    else:
+        h_out = h
     if out is None:
-        out = _alloc(h.shape, ytype, h, stream)
-    elif out.shape != h.shape or out.dtype is not ytype or not out.is_contiguous():
+        out = _alloc_like(y, stream) if yp and ypitch == d else _alloc(shape, ytype, h, stream)
+    elif out.shape != shape or out.dtype is not ytype or not out.is_contiguous():
         _bad("out must be contiguous, of h's shape and y's type")
-    for v, what in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
-                    (pre_bias, "pre_bias")):
-        if v is not None:
-            _vector(v, d, what)
-    _on_device(h, y, post_weight, post_bias, pre_weight, pre_bias, gate, h_out, out)
+    elif out.get_device() != dev:
+        _elsewhere(out)
+    if post_weight is not None:
+        a = _vector(post_weight, d, dev, "post_weight")
+    if post_bias is not None:
+        b = _vector(post_bias, d, dev, "post_bias")
+    if pre_weight is not None:
+        c = _vector(pre_weight, d, dev, "pre_weight")
+    if pre_bias is not None:
+        e = _vector(pre_bias, d, dev, "pre_bias")
     s = _pack_norms(kind, hkind, r, d, _NORMS[norm], 1 if post else 0, gates, eps, alpha, beta, hpitch, ypitch)
-    _check(_fn("qnn_lm_norm_residual")(s, h.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight),
-                                       _ptr(pre_bias), _ptr(gate), _ptr(h_out) if y is not None else None,
-                                       out.data_ptr(), qnn._stream_int(stream)), "qnn_lm_norm_residual")
-    return (h if y is None else h_out), out
+    status = (_f or _load())["qnn_lm_norm_residual"](s, h.data_ptr(), yp, a, b, c, e, gp, hop, out.data_ptr(), handle)
+    if status:
+        raise QnnError(status, "qnn_lm_norm_residual")
+    return h_out, out
 
 
 def make_cache(pages, heads, page, dim, bits, dtype=torch.bfloat16, device="cuda"):
@@ -240,34 +301,42 @@ def make_cache(pages, heads, page, dim, bits, dtype=torch.bfloat16, device="cuda
     return Cache(k, v, ks, vs, bits)
 
 
-def _cache(cache, table, b):
-    """(the C structure, heads, dim, number type or None at fewer bits)"""
+def _cache(cache, table, b, d):
+    """(the C structure, heads, dim, the numbers' type at 16 bits or None); d: the device."""
     k, v, ks, vs, bits = cache
-    if k.dim() != 4 or k.shape != v.shape or k.dtype is not v.dtype:
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
         _bad("k and v of a cache must be [pages, heads, page, dim], alike")
-    pages, heads, page, width = k.shape
-    if bits == 16:
-        kind = _TYPES.get(k.dtype, F32)
-        if kind == F32:
-            _bad("a cache of 16 bits holds bfloat16 or float16")
-        unit, dim = 2, width
-    else:
-        if k.dtype is not torch.uint8 or bits not in (8, 4):
-            _bad("a cache holds uint8 codes of 8 or 4 bits, or numbers of 16 bits")
-        kind, unit, dim = BF16, 1, width * 8 // bits
-        for s in (ks, vs):
-            if s is None or s.dtype is not torch.float32 or s.shape != k.shape[:3] or not s.is_contiguous():
-                _bad("the scales of a cache must be contiguous float32 [pages, heads, page]")
-    a, c = k.stride(), v.stride()
-    if a[3] != 1 or c[3] != 1:
+    pages, heads, page, dim = shape
+    a0, a1, a2, a3 = k.stride()
+    c0, c1, c2, c3 = v.stride()
+    if a3 != 1 or c3 != 1:
         _bad("the channels of a cache must be contiguous")
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != b or not table.is_contiguous():
+    ksp = vsp = 0
+    if bits == 16:
+        kind = _TYPES16.get(dtype)
+        if kind is None or ks is not None or vs is not None:
+            _bad("a cache of 16 bits holds bfloat16 or float16 and no scales")
+        a0, a1, a2, c0, c1, c2 = 2 * a0, 2 * a1, 2 * a2, 2 * c0, 2 * c1, 2 * c2
+    else:
+        if dtype is not _U8 or (bits != 8 and bits != 4):
+            _bad("a cache holds uint8 codes of 8 or 4 bits, or numbers of 16 bits")
+        kind, dtype = 0, None
+        if bits == 4:
+            dim *= 2
+        for s in (ks, vs):
+            if s is None or s.dtype is not _F32 or s.shape != shape[:3] or not s.is_contiguous():
+                _bad("the scales of a cache must be contiguous float32 [pages, heads, page]")
+            if s.get_device() != d:
+                _elsewhere(s)
+        ksp, vsp = ks.data_ptr(), vs.data_ptr()
+    t = table.shape
+    if len(t) != 2 or t[0] != b or table.dtype is not _I32 or not table.is_contiguous():
         _bad("table must be contiguous int32 [%d, pages of a sequence]" % b)
-    _on_device(k, v, ks, vs, table)
-    return (_pack_cache(kind, bits, pages, heads, page, dim, a[0] * unit, a[1] * unit, a[2] * unit, c[0] * unit,
-                        c[1] * unit, c[2] * unit, k.data_ptr(), v.data_ptr(), ks.data_ptr() if ks is not None else 0,
-                        vs.data_ptr() if vs is not None else 0, table.data_ptr(), b, table.shape[1]),
-            heads, dim, k.dtype if bits == 16 else None)
+    if k.get_device() != d or v.get_device() != d or table.get_device() != d:
+        _bad("the cache and its table must be on the other tensors' device")
+    return (_pack_cache(kind, bits, pages, heads, page, dim, a0, a1, a2, c0, c1, c2, k.data_ptr(), v.data_ptr(), ksp, vsp,
+                        table.data_ptr(), b, t[1]), heads, dim, dtype)
 
 
 def tree_attention(q, cache, table, lens, mask=None, counts=None, scale=None, out=None, want_lse=False, stream=None):
@@ -281,32 +350,50 @@ def tree_attention(q, cache, table, lens, mask=None, counts=None, scale=None, ou
     a prompt; t = 1: plain decoding).  scale: of the scores, 1 / sqrt(dim) if
     not given.  Returns [b, t, heads, dim], with want_lse also float32
     [b, t, heads]."""
-    if q.dim() != 4 or q.stride(3) != 1:
+    st = q.stride()
+    if len(st) != 4 or st[3] != 1:
         _bad("q must be [b, t, heads, dim], contiguous along dim")
-    b, t, heads, dim = q.shape
-    kind = _TYPES.get(q.dtype, F32)
-    c, _, cdim, ctype = _cache(cache, table, b)
-    if kind == F32 or (ctype is not None and ctype is not q.dtype):
+    shape = q.shape
+    b, t, heads, dim = shape
+    dtype = q.dtype
+    kind = _TYPES16.get(dtype)
+    d = q.get_device()
+    c, _, cdim, ctype = _cache(cache, table, b, d)
+    if kind is None or (ctype is not None and ctype is not dtype):
         _bad("q must be bfloat16 or float16, and of the type of a cache of 16 bits")
     if cdim != dim:
         _bad("q has heads of %d channels, the cache of %d" % (dim, cdim))
-    _ints(lens, (b,), "lens")
-    _ints(counts, (b,), "counts")
-    if mask is not None and (mask.dtype is not torch.int64 or tuple(mask.shape) != (b, t, (t + 63) // 64)
-                             or not mask.is_contiguous()):
-        _bad("mask must be contiguous int64 [b, t, ceil(t / 64)]")
+    handle = _stream(d, stream)
+    lp = _ints(lens, b, d, "lens")
+    cp = mp = sp = None
+    if counts is not None:
+        cp = _ints(counts, b, d, "counts")
+    if mask is not None:
+        if mask.dtype is not torch.int64 or mask.shape != (b, t, (t + 63) // 64) or not mask.is_contiguous():
+            _bad("mask must be contiguous int64 [b, t, ceil(t / 64)]")
+        if mask.get_device() != d:
+            _elsewhere(mask)
+        mp = mask.data_ptr()
     if out is None:
-        out = _alloc((b, t, heads, dim), q.dtype, q, stream)
-    elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_contiguous():
+        out = _alloc_like(q, stream) if q.is_contiguous() else _alloc(shape, dtype, q, stream)
+    elif out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
         _bad("out must be contiguous and like q")
-    lse = _alloc((b, t, heads), torch.float32, q, stream) if want_lse else None
-    _on_device(q, lens, counts, mask, out)
-    st = q.stride()
-    s = _pack_queries(kind, t, heads, 1 / math.sqrt(dim) if scale is None else scale, st[0], st[1], st[2])
-    size = _fn("qnn_lm_tree_attention_workspace")(s, c)
-    ws = _alloc((size,), torch.uint8, q, stream) if size else None
-    _check(_f["qnn_lm_tree_attention"](s, q.data_ptr(), c, lens.data_ptr(), _ptr(counts), _ptr(mask), out.data_ptr(),
-                                       _ptr(lse), _ptr(ws), size, qnn._stream_int(stream)), "qnn_lm_tree_attention")
+    elif out.get_device() != d:
+        _elsewhere(out)
+    lse = None
+    if want_lse:
+        lse = _alloc(shape[:3], _F32, q, stream)
+        sp = lse.data_ptr()
+    s = _pack_queries(kind, t, heads, dim ** -0.5 if scale is None else scale, st[0], st[1], st[2])
+    f = _f or _load()
+    size = f["qnn_lm_tree_attention_workspace"](s, c)
+    ws = wp = None
+    if size:
+        ws = _alloc(size, _U8, q, stream)
+        wp = ws.data_ptr()
+    status = f["qnn_lm_tree_attention"](s, q.data_ptr(), c, lp, cp, mp, out.data_ptr(), sp, wp, size, handle)
+    if status:
+        raise QnnError(status, "qnn_lm_tree_attention")
     return (out, lse) if want_lse else out
 
 
@@ -314,38 +401,44 @@ def cache_append(k, v, cache, table, lens, counts=None, stream=None):
     """Writes new tokens into the cache (qnn_lm_cache_append): k and v
     [b, t, heads, dim] bfloat16 or float16, token j of a sequence to position
     lens + j where j < counts (None: t)."""
-    if k.dim() != 4 or k.shape != v.shape or k.dtype is not v.dtype or k.stride(3) != 1 or v.stride(3) != 1:
-        _bad("k and v must be [b, t, heads, dim], alike, contiguous along dim")
-    b, t, heads, dim = k.shape
-    kind = _TYPES.get(k.dtype, F32)
-    c, cheads, cdim, ctype = _cache(cache, table, b)
-    if kind == F32 or (ctype is not None and ctype is not k.dtype):
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
+        _bad("k and v must be [b, t, heads, dim], alike")
+    a0, a1, a2, a3 = k.stride()
+    c0, c1, c2, c3 = v.stride()
+    if a3 != 1 or c3 != 1:
+        _bad("k and v must be contiguous along dim")
+    b, t, heads, dim = shape
+    kind = _TYPES16.get(dtype)
+    d = k.get_device()
+    c, cheads, cdim, ctype = _cache(cache, table, b, d)
+    if kind is None or (ctype is not None and ctype is not dtype):
         _bad("k and v must be bfloat16 or float16, and of the type of a cache of 16 bits")
-    if (heads, dim) != (cheads, cdim):
+    if heads != cheads or dim != cdim:
         _bad("k and v have %d heads of %d channels, the cache %d of %d" % (heads, dim, cheads, cdim))
-    _ints(lens, (b,), "lens")
-    _ints(counts, (b,), "counts")
-    _on_device(k, v, lens, counts)
-    a, d = k.stride(), v.stride()
-    s = _pack_tokens(kind, t, a[0], a[1], a[2], d[0], d[1], d[2])
-    _check(_fn("qnn_lm_cache_append")(s, k.data_ptr(), v.data_ptr(), c, lens.data_ptr(), _ptr(counts),
-                                      qnn._stream_int(stream)), "qnn_lm_cache_append")
+    if v.get_device() != d:
+        _elsewhere(v)
+    s = _pack_tokens(kind, t, a0, a1, a2, c0, c1, c2)
+    status = (_f or _load())["qnn_lm_cache_append"](
+        s, k.data_ptr(), v.data_ptr(), c, _ints(lens, b, d, "lens"),
+        None if counts is None else _ints(counts, b, d, "counts"), _stream(d, stream))
+    if status:
+        raise QnnError(status, "qnn_lm_cache_append")
 
 
 def cache_keep(cache, table, lens, path, kept, stream=None):
     """Moves the accepted drafts to the front (qnn_lm_cache_keep): position
     lens + j takes position lens + path[:, j] for j < kept.  path: int32 [b, t],
     strictly ascending; kept: int32 [b]."""
-    if path.dim() != 2:
-        _bad("path must be [b, t]")
+    if path.dim() != 2 or path.dtype is not _I32 or not path.is_contiguous():
+        _bad("path must be contiguous int32 [b, t]")
     b, t = path.shape
-    c = _cache(cache, table, b)[0]
-    _ints(path, (b, t), "path")
-    _ints(lens, (b,), "lens")
-    _ints(kept, (b,), "kept")
-    _on_device(lens, path, kept)
-    _check(_fn("qnn_lm_cache_keep")(c, t, lens.data_ptr(), path.data_ptr(), kept.data_ptr(), qnn._stream_int(stream)),
-           "qnn_lm_cache_keep")
+    d = path.get_device()
+    status = (_f or _load())["qnn_lm_cache_keep"](
+        _cache(cache, table, b, d)[0], t, _ints(lens, b, d, "lens"), path.data_ptr(), _ints(kept, b, d, "kept"),
+        _stream(d, stream))
+    if status:
+        raise QnnError(status, "qnn_lm_cache_keep")
 
 
 def cache_read(cache, table, start, n, dtype=torch.bfloat16, stream=None):
@@ -355,12 +448,12 @@ def cache_read(cache, table, start, n, dtype=torch.bfloat16, stream=None):
     kind = _TYPES.get(dtype)
     if kind is None:
         _bad("dtype must be bfloat16, float16 or float32")
-    b = start.shape[0]
-    c, heads, dim, _ = _cache(cache, table, b)
-    _ints(start, (b,), "start")
-    _on_device(start)
+    b, d = start.numel(), start.get_device()
+    c, heads, dim, _ = _cache(cache, table, b, d)
+    sp, handle = _ints(start, b, d, "start"), _stream(d, stream)
     k = _alloc((b, n, heads, dim), dtype, start, stream)
-    v = _alloc((b, n, heads, dim), dtype, start, stream)
-    _check(_fn("qnn_lm_cache_read")(c, kind, n, start.data_ptr(), k.data_ptr(), v.data_ptr(), qnn._stream_int(stream)),
-           "qnn_lm_cache_read")
+    v = _alloc_like(k, stream)
+    status = (_f or _load())["qnn_lm_cache_read"](c, kind, n, sp, k.data_ptr(), v.data_ptr(), handle)
+    if status:
+        raise QnnError(status, "qnn_lm_cache_read")
     return k, v
