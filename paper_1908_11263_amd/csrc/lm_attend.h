@@ -3,15 +3,14 @@
 // and sum of the softmax.
 //
 // The rows of a cache head are its query heads times the drafts: row = draft *
-// g + query head of the group.  A workgroup owns 16 NR rows of one head of one
-// sequence and one piece of its positions; its four waves take tiles of 32
-// positions in turn, each with its own maximum, sum and outputs, joined through
-// local memory at the end: no barrier in the loop.  Pieces are joined by a
-// second kernel.
+// g + query head of the group.  A workgroup owns some rows of one head of one
+// sequence and one piece of its positions.  With few rows its waves share out
+// the positions (lm_attend_few.h), with many the rows (lm_attend_many.h).
+// Pieces are joined by a second kernel.
 //
 // Both products are taken transposed on the 16x16x32 matrix instruction, so
 // that a lane keeps one row's statistics and never passes a probability on:
-//   S^T = K Q^T  (A = 16 positions of K, straight from memory; B = Q): lane l
+//   S^T = K Q^T  (A = 16 positions of K; B = Q): lane l
 //         gets row l % 16 at positions 4 * (l / 16) .. + 3;
 //   O^T = V^T P^T (B = P): lane l's eight k's are the positions that it holds
 //         of the tile's two halves, in the order that A uses as well;
@@ -25,450 +24,99 @@
 namespace qnn_lm {
 
 typedef short s4_ __attribute__((ext_vector_type(4)));
+typedef short s8_ __attribute__((ext_vector_type(8)));
 typedef int i2_ __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s4_ lds_s4;
 typedef __attribute__((address_space(3))) i2_ lds_i2;
 
-constexpr int kAttendTile = 32;  // positions of a tile
-
 struct AttendPlan {
     int32_t g;          // query heads of a cache head
     int32_t rows;       // t * g
-    int32_t row_tiles;  // of 16 NR rows
+    int32_t many;       // the waves share out the rows
+    int32_t nr;         // sixteens of rows of a wave
+    int32_t row_tiles;  // of 16 nr rows, or of 64 nr
     int32_t splits;     // pieces of the positions
     int32_t shift;      // page = 1 << shift, or -1
     float *part;        // [splits][b][t][heads][dim] outputs, then their maxima and sums
 };
 
-template <int BITS, int DIM>
-struct KvShape {
-    static constexpr int kPiece = (128 / BITS < DIM / 4) ? 128 / BITS : DIM / 4;  // codes of a lane's load of K
-    static constexpr int kLoads = DIM / (4 * kPiece);
-    static constexpr int kWords = kPiece * BITS / 32;
-    static constexpr int kSub = kPiece / 8;          // eights of a load
-    static constexpr int kRow = DIM * BITS / 8;      // bytes of a slot
-    static constexpr int kStaged = BITS == 16 ? 2 * DIM : DIM;  // bytes of a staged row of V
-    static constexpr int kVLane = BITS == 4 ? 8 : 16;  // bytes of a lane's load of V
-    static constexpr int kVLanes = kRow / kVLane;      // lanes of a row
-    static constexpr int kVLoads = kAttendTile * kVLanes / 64;
-    static constexpr int kVWords = kVLane / 4;
-    // rows are set off so that the transposing reads, 16 or 32 rows at a time,
-    // spread over the banks
-    static constexpr int kPitch = kStaged + (BITS == 16 ? 32 : 16);
-    static constexpr int kWaveLds = kAttendTile * kPitch + 3 * kAttendTile * 4;
-};
-
-// One tile's K and V in flight.
-template <int BITS, int DIM>
-struct KvTile {
-    using S = KvShape<BITS, DIM>;
-    uint32_t k[2][S::kLoads][S::kWords];
-    uint32_t v[S::kVLoads][S::kVWords];
-    float ks, vs;     // of position lane % 32
-    uint32_t valid;   // positions that are in the cache and before the end
-
-    __device__ __forceinline__ void load(const CacheArgs &c, int shift, int32_t seq, int32_t head, int32_t p0,
-                                         int32_t end, int lane)
+// Sequence's lengths, bounded.
+struct AttendSeq {
+    int32_t len, count;
+    __device__ __forceinline__ AttendSeq(const AttendArgs &a, int32_t seq)
     {
-        const int l32 = lane & 31;
-        // lane l % 32 looks its position up; the others take it from there
-        Slot s = {-1, 0};
-        const int32_t pos = p0 + l32;
-        if (pos < end) {
-            const int32_t pg = shift >= 0 ? pos >> shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
-            const int32_t page = c.table[(int64_t)seq * c.width + pg];
-            if ((uint32_t)page < (uint32_t)c.pages) {
-                s.page = page;
-                s.slot = pos - pg * c.page;
-            }
-        }
-        valid = (uint32_t)__ballot(s.page >= 0);
-        if constexpr (BITS != 16) {
-            ks = vs = 0.f;
-            if (s.page >= 0) {
-                const int64_t at = scale_at(c, s, head);
-                ks = c.k_scale[at];
-                vs = c.v_scale[at];
-            }
-        }
-        const int l16 = lane & 15, kq = lane >> 4;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int32_t page = __shfl(s.page, 16 * u + l16, 64), slot = __shfl(s.slot, 16 * u + l16, 64);
-            const uint8_t *p = c.k + page * c.k_page + head * c.k_head + slot * c.k_slot;
-#pragma unroll
-            for (int i = 0; i < S::kLoads; ++i) {
-#pragma unroll
-                for (uint32_t &w : k[u][i])
-                    w = 0;
-                if (page >= 0)
-                    load_words<S::kWords>(p + (i * 4 + kq) * (S::kWords * 4), k[u][i]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < S::kVLoads; ++i) {
-            const int row = i * (64 / S::kVLanes) + lane / S::kVLanes;
-            const int32_t page = __shfl(s.page, row, 64), slot = __shfl(s.slot, row, 64);
-#pragma unroll
-            for (uint32_t &w : v[i])
-                w = 0;
-            if (page >= 0)
-                load_words<S::kVWords>(c.v + page * c.v_page + head * c.v_head + slot * c.v_slot +
-                                           (lane % S::kVLanes) * S::kVLane,
-                                       v[i]);
-        }
+        len = max(a.lens[seq], 0);
+        count = a.counts ? min(max(a.counts[seq], 0), a.t) : a.t;
     }
-
-    // s[n][u] += the I-th and later products of half u's keys with the queries
-    template <class N, int I, int NR>
-    __device__ __forceinline__ void scores(int u, const typename N::V8 (&q)[NR][DIM / 32], f4 (&s)[NR][2]) const
+    // Positions that rows row0 .. row0 + rows - 1 can see end here.
+    __device__ __forceinline__ int32_t end(const AttendArgs &a, const CacheArgs &c, const AttendPlan &p, int32_t row0,
+                                           int32_t rows) const
     {
-        if constexpr (I < DIM / 32) {
-            const typename N::V8 kf = expand<N, BITS, I % S::kSub>(k[u][I / S::kSub]);
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-                s[n][u] = mfma16(kf, q[n][I], s[n][u]);
-            scores<N, I + 1, NR>(u, q, s);
-        }
-    }
-
-    // V's rows into this wave's local memory, 4-bit codes as bytes (16 times the code).
-    __device__ __forceinline__ void stage(uint8_t *lds, int lane) const
-    {
-#pragma unroll
-        for (int i = 0; i < S::kVLoads; ++i) {
-            const int row = i * (64 / S::kVLanes) + lane / S::kVLanes;
-            uint8_t *p = lds + row * S::kPitch + (lane % S::kVLanes) * 16;
-            u4 r;
-            if constexpr (BITS == 4) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t lo = (v[i][h] << 4) & 0xF0F0F0F0u, hi = v[i][h] & 0xF0F0F0F0u;
-                    r[2 * h] = __builtin_amdgcn_perm(hi, lo, 0x05010400u);
-                    r[2 * h + 1] = __builtin_amdgcn_perm(hi, lo, 0x07030602u);
-                }
-            } else {
-                r = (u4){v[i][0], v[i][1], v[i][2], v[i][3]};
-            }
-            *(u4 *)p = r;
-        }
-    }
-
-    // Whether a 16-bit value of the tile is infinite or NaN.
-    template <class N>
-    __device__ __forceinline__ bool odd_values() const
-    {
-        constexpr uint32_t e = __is_same(N, Bf16) ? 0x7F80u : 0x7C00u;
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < S::kVLoads; ++i)
-#pragma unroll
-            for (uint32_t w : v[i])
-                odd |= (w & e) == e || ((w >> 16) & e) == e;
-        return __any(odd);
+        const int32_t last = min(count, (min(row0 + rows, p.rows) - 1) / p.g + 1);
+        const int32_t seen = row0 / p.g >= count ? 0 : a.mask ? count : last;
+        return seen ? (int32_t)min((int64_t)len + seen, (int64_t)c.width * c.page) : 0;
     }
 };
 
-// The eight values of V^T at channel 16 * block + l % 16: positions 4 * (l /
-// 16) .. + 3 of the tile's first half, then of its second.
-template <class N, int BITS, int DIM>
-__device__ __forceinline__ typename N::V8 value_frag(const uint8_t *lds, int block, int lane)
+// Which of the 64 positions from p0 on draft i sees, as bits (cached tokens:
+// all; whether a position is in the cache at all is not asked).
+__device__ __forceinline__ uint64_t seen_bits(const AttendArgs &a, int32_t seq, int32_t i, int64_t p0, int32_t len)
 {
-    using S = KvShape<BITS, DIM>;
-    const int l16 = lane & 15, kq = lane >> 4;
-    if constexpr (BITS == 16) {
-        const uint8_t *p = lds + (4 * kq + (l16 >> 2)) * S::kPitch + block * 32 + (l16 & 3) * 8;
-        const s4_ a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p);
-        const s4_ b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 16 * S::kPitch));
-        typedef short s8_ __attribute__((ext_vector_type(8)));
-        const s8_ r = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        return __builtin_bit_cast(typename N::V8, r);
+    const int64_t j0 = p0 - len;  // draft of the first bit
+    if (j0 <= -64)
+        return ~0ull;
+    if (!a.mask) {
+        const int64_t n = i - j0 + 1;
+        return n >= 64 ? ~0ull : n <= 0 ? 0 : (1ull << n) - 1;
+    }
+    const int32_t words = (a.t + 63) >> 6, w = (int32_t)(j0 >> 6), s = (int32_t)j0 & 63;
+    const uint64_t *row = a.mask + ((int64_t)seq * a.t + i) * words;
+    const uint64_t lo = w < 0 ? ~0ull : w < words ? row[w] : 0, hi = w + 1 < words ? row[w + 1] : 0;
+    return s ? lo >> s | hi << (64 - s) : lo;
+}
+
+// A row's result from its sum l, maximum m (in powers of two) and outputs
+// v = 4 channels at d: into the pieces, or finished.
+template <class N, int DIM>
+__device__ __forceinline__ void store_row(const AttendArgs &a, const AttendPlan &p, int64_t all, int32_t split,
+                                          int64_t index, int d, f4 v, float inv)
+{
+    if (p.splits > 1) {
+        *(f4 *)(p.part + (split * all + index) * DIM + d) = v;
     } else {
-        const int row = 4 * kq + ((l16 >> 1) & 3) + 16 * (l16 >> 3);
-        const uint8_t *p = lds + row * S::kPitch + block * 16 + (l16 & 1) * 8;
-        const i2_ a = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2 *)p);
-        return expand_bytes<N>((uint32_t)a.x, (uint32_t)a.y);
+        const u2 r = {pack2<N>(v[0] * inv, v[1] * inv), pack2<N>(v[2] * inv, v[3] * inv)};
+        *(u2 *)((typename N::T *)a.out + index * DIM + d) = r;
     }
 }
 
-template <class N, int BITS, int DIM, int NR>
-__global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, AttendPlan pl)
+template <int DIM>
+__device__ __forceinline__ void store_stats(const AttendArgs &a, const AttendPlan &p, int64_t all, int32_t split,
+                                            int64_t index, float m, float l)
 {
-    using S = KvShape<BITS, DIM>;
-    constexpr int ND = DIM / 16, NK = DIM / 32;
-    extern __shared__ __align__(16) uint8_t lds[];
-    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t split = blockIdx.x % pl.splits, tile = blockIdx.x / pl.splits;
-    const int32_t head = blockIdx.y, seq = blockIdx.z;
-    const int32_t len = max(a.lens[seq], 0);
-    const int32_t count = a.counts ? min(max(a.counts[seq], 0), a.t) : a.t;
-    const int32_t row0 = tile * 16 * NR;
-    // positions that a row of this tile can see end here
-    const int32_t last_draft = min(count, (min(row0 + 16 * NR, pl.rows) - 1) / pl.g + 1);
-    const int32_t seen = row0 / pl.g >= count ? 0 : a.mask ? count : last_draft;
-    const int64_t reach = (int64_t)c.width * c.page;
-    const int32_t end = seen ? (int32_t)min((int64_t)len + seen, reach) : 0;
-
-    // this lane's rows: queries and draft numbers
-    typename N::V8 q[NR][NK];
-    int32_t draft[NR];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        const int32_t row = row0 + n * 16 + l16;
-        draft[n] = row < pl.rows ? row / pl.g : -1;
-        const bool live = draft[n] >= 0 && draft[n] < count;
-        const typename N::T *p = (const typename N::T *)a.q + seq * a.q_b + max(draft[n], 0) * a.q_t +
-                                 (head * pl.g + (live ? row - draft[n] * pl.g : 0)) * a.q_h;
-        if (!live)
-            draft[n] = -1;
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            // the channels that K's lane loads put into product i
-            const int d = (i / S::kSub) * 4 * S::kPiece + kq * S::kPiece + (i % S::kSub) * 8;
-            u4 v = {0, 0, 0, 0};
-            if (live)
-                v = *(const u4 *)(p + d);
-            q[n][i] = __builtin_bit_cast(typename N::V8, v);
-        }
-    }
-    f4 o[NR][ND];
-    float m[NR], l[NR];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        m[n] = -INFINITY;
-        l[n] = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-            o[n][d] = (f4){0, 0, 0, 0};
-    }
-    const float qs = a.scale * 1.44269504088896f * (BITS == 4 ? 1.f / 16 : 1.f);  // scores in powers of two
-    // f16 only: values' scales are taken relative to 2^vexp, so that the
-    // probabilities that they multiply stay normal numbers
-    int vexp = -1000;
-    uint8_t *vl = lds + wave * S::kWaveLds;
-    float *scales = (float *)(vl + kAttendTile * S::kPitch);
-
-    const int32_t tiles = (end + kAttendTile - 1) / kAttendTile;
-    const int32_t share = (tiles + pl.splits - 1) / pl.splits;
-    const int32_t last = min((split + 1) * share, tiles);
-    int32_t at = split * share + wave;
-    KvTile<BITS, DIM> cur, next;
-    if (at < last)
-        cur.load(c, pl.shift, seq, head, at * kAttendTile, end, lane);
-    for (; at < last; at += 4) {
-        if (at + 4 < last)
-            next.load(c, pl.shift, seq, head, (at + 4) * kAttendTile, end, lane);
-        const int32_t p0 = at * kAttendTile;
-        cur.stage(vl, lane);
-        if constexpr (BITS != 16) {
-            float vs = cur.vs * (BITS == 4 ? 1.f / 16 : 1.f);
-            if constexpr (__is_same(N, F16)) {
-                // (scales that are not finite stay so)
-                int e = vs > 0.f && vs < INFINITY ? ilogbf(vs) : -1000;
-#pragma unroll
-                for (int s = 1; s < 32; s <<= 1)
-                    e = max(e, __shfl_xor(e, s, 64));
-                if (e > vexp) {
-                    const float f = ldexpf(1.f, max(vexp - e, -300));
-#pragma unroll
-                    for (int n = 0; n < NR; ++n)
-#pragma unroll
-                        for (int d = 0; d < ND; ++d)
-                            o[n][d] *= f;
-                    vexp = e;
-                }
-                vs = ldexpf(vs, -vexp);
-            }
-            if (lane < 32) {
-                scales[lane] = cur.ks * qs;
-                scales[32 + lane] = vs;
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        f4 ks[2], vs[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if constexpr (BITS != 16) {
-                ks[u] = *(const f4 *)(scales + 16 * u + 4 * kq);
-                vs[u] = *(const f4 *)(scales + 32 + 16 * u + 4 * kq);
-            } else {
-                ks[u] = (f4){qs, qs, qs, qs};
-                vs[u] = (f4){1, 1, 1, 1};
-            }
-        }
-        f4 s[NR][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-                s[n][u] = (f4){0, 0, 0, 0};
-            cur.template scores<N, 0>(u, q, s);
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-                s[n][u] *= ks[u];
-        }
-        const bool whole = cur.valid == 0xFFFFFFFFu && p0 + kAttendTile <= len;
-        if (!whole) {
-            const int32_t words = (a.t + 63) >> 6;
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int at32 = 16 * u + 4 * kq + i;
-                        const int32_t j = p0 + at32 - len;  // < 0: before the drafts
-                        bool see = ((cur.valid >> at32) & 1) && draft[n] >= 0;
-                        if (see && j >= 0)
-                            see = a.mask ? (a.mask[((int64_t)seq * a.t + draft[n]) * words + (j >> 6)] >> (j & 63)) & 1
-                                         : j <= draft[n];
-                        if (!see)
-                            s[n][u][i] = -INFINITY;
-                    }
-        }
-        typename N::V8 p[NR];
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
-                              fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            if (__any(top > m[n])) {
-                const float mn = fmaxf(m[n], top);
-                // (rows that have seen nothing: 2^(-inf) = 0, of zeros)
-                const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - mn);
-                m[n] = mn;
-                l[n] *= f;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-                    o[n][d] *= f;
-            }
-            const float mm = m[n] == -INFINITY ? 0.f : m[n];
-            float e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                e[i] = __builtin_amdgcn_exp2f(s[n][i / 4][i % 4] - mm);
-                l[n] += e[i];
-                // (a select: what an unseen position's scale holds has no influence)
-                if constexpr (BITS != 16)
-                    e[i] = whole || s[n][i / 4][i % 4] != -INFINITY ? e[i] * vs[i / 4][i % 4] : 0.f;
-            }
-            const u4 r = {pack2<N>(e[0], e[1]), pack2<N>(e[2], e[3]), pack2<N>(e[4], e[5]), pack2<N>(e[6], e[7])};
-            p[n] = __builtin_bit_cast(typename N::V8, r);
-        }
-        bool odd = false;
-        if constexpr (BITS == 16)
-            odd = !whole && cur.template odd_values<N>();
-        if (!odd) {
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const typename N::V8 vf = value_frag<N, BITS, DIM>(vl, d, lane);
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-                    o[n][d] = mfma16(vf, p[n], o[n][d]);
-            }
-        } else if constexpr (BITS == 16) {
-            // an infinite or NaN value that some row does not see: one
-            // position at a time, only where it is seen
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    for (int from = 0; from < 4; ++from) {
-                        const float pe = __shfl((float)p[n][e], from * 16 + l16, 64);
-                        const float se = __shfl(s[n][e / 4][e % 4], from * 16 + l16, 64);
-                        const uint8_t *vr = vl + (16 * (e / 4) + 4 * from + e % 4) * S::kPitch;
-                        if (se == -INFINITY)
-                            continue;
-#pragma unroll
-                        for (int d = 0; d < ND; ++d)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                o[n][d][i] += pe * load1<N>(vr, d * 16 + 4 * kq + i);
-                    }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        cur = next;
-    }
-    // join the four waves, sixteen rows at a time
-    constexpr int OP = DIM + 4;  // pitch in floats
-    float *jo = (float *)lds, *jm = jo + 4 * 16 * OP, *jl = jm + 64;
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        l[n] += __shfl_xor(l[n], 16, 64);
-        l[n] += __shfl_xor(l[n], 32, 64);
-        if (draft[n] < 0)
-            m[n] = -INFINITY;  // no draft of this sequence: has seen nothing
-        __syncthreads();
-        if (kq == 0) {
-            jm[wave * 16 + l16] = m[n];
-            jl[wave * 16 + l16] = l[n];
-        }
-        __syncthreads();
-        float top = jm[l16];
-#pragma unroll
-        for (int w = 1; w < 4; ++w)
-            top = fmaxf(top, jm[w * 16 + l16]);
-        float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - top);
-        // (a wave that saw no scale has no outputs either)
-        if (BITS != 16 && __is_same(N, F16))
-            f = vexp == -1000 ? 0.f : ldexpf(f, vexp);
-        if (m[n] == -INFINITY)
-            f = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = o[n][d] * f;
-        __syncthreads();
-        // 16 threads a row
-        const int r = threadIdx.x >> 4, e0 = threadIdx.x & 15;
-        const int32_t row = row0 + n * 16 + r;
-        if (row < pl.rows) {
-            float mt = jm[r];
-#pragma unroll
-            for (int w = 1; w < 4; ++w)
-                mt = fmaxf(mt, jm[w * 16 + r]);
-            float lt = 0.f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-                lt += jm[w * 16 + r] == -INFINITY ? 0.f : jl[w * 16 + r] * __builtin_amdgcn_exp2f(jm[w * 16 + r] - mt);
-            const int32_t dr = row / pl.g, hq = head * pl.g + row - dr * pl.g;
-            const int64_t index = ((int64_t)seq * a.t + dr) * a.heads + hq;
-            const int64_t all = (int64_t)c.b * a.t * a.heads;
-            const float inv = pl.splits > 1 ? 1.f : (mt == -INFINITY ? 0.f : 1.f / lt);
-            for (int e = e0 * 8; e < DIM; e += 128) {
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float t = 0.f;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        t += jo[(w * 16 + r) * OP + e + i];
-                    v[i] = mt == -INFINITY ? 0.f : t * inv;
-                }
-                if (pl.splits > 1)
-                    store8<F32>(pl.part, (split * all + index) * DIM + e, v);
-                else
-                    store8<N>(a.out, index * DIM + e, v);
-            }
-            if (e0 == 0) {
-                if (pl.splits > 1) {
-                    float *ml = pl.part + pl.splits * all * DIM + (split * all + index) * 2;
-                    ml[0] = mt;
-                    ml[1] = lt;
-                } else if (a.lse) {
-                    a.lse[index] = mt == -INFINITY ? -INFINITY : 0.693147180559945f * (mt + log2f(lt));
-                }
-            }
-        }
+    if (p.splits > 1) {
+        float *ml = p.part + p.splits * all * DIM + (split * all + index) * 2;
+        ml[0] = m;
+        ml[1] = l;
+    } else if (a.lse) {
+        a.lse[index] = m == -INFINITY ? -INFINITY : 0.693147180559945f * (m + log2f(l));
     }
 }
 
-hipError_t launch_attend_bf16(const AttendArgs &a, const CacheArgs &c, const AttendPlan &p, int bits, int dim, int nr,
+// Largest exponent of the scales that lanes hold (-1000 where all are zero or
+// not finite).
+template <int LANES>
+__device__ __forceinline__ int scale_exponent(float v)
+{
+    int e = v > 0.f && v < INFINITY ? ilogbf(v) : -1000;
+#pragma unroll
+    for (int s = 1; s < LANES; s <<= 1)
+        e = max(e, __shfl_xor(e, s, 64));
+    return __builtin_amdgcn_readfirstlane(e);
+}
+
+hipError_t launch_attend_bf16(const AttendArgs &a, const CacheArgs &c, const AttendPlan &p, int bits, int dim,
                               hipStream_t s);
-hipError_t launch_attend_f16(const AttendArgs &a, const CacheArgs &c, const AttendPlan &p, int bits, int dim, int nr,
+hipError_t launch_attend_f16(const AttendArgs &a, const CacheArgs &c, const AttendPlan &p, int bits, int dim,
                              hipStream_t s);
 
 }  // namespace qnn_lm

@@ -40,18 +40,20 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part, void *out,
         lse[row] = m == -INFINITY ? -INFINITY : 0.693147180559945f * (m + log2f(l));
 }
 
-// Rows a workgroup and pieces of the positions.  Few rows take the smallest
-// tile that holds them; positions are split until there are two workgroups for
-// each of the 256 compute units, in pieces of at least 128 positions (one tile
-// a wave).  Lengths live on the device: the plan goes by what the table can
-// reach, the kernel shares out the positions that there are.
-static AttendPlan plan_attend(const AttendArgs &a, const CacheArgs &c, int dim, int *nr)
+// Rows a workgroup and pieces of the positions.  Up to 32 rows go to the kernel
+// whose waves share out the positions.  Positions are split until there are two
+// workgroups for each of the 256 compute units, in pieces of at least 128
+// positions.  Lengths live on the device: the plan goes by what the table can
+// reach, the kernels share out the positions that there are.
+static AttendPlan plan_attend(const AttendArgs &a, const CacheArgs &c, int dim)
 {
     AttendPlan p;
     p.g = a.heads / c.heads;
     p.rows = a.t * p.g;
-    *nr = p.rows <= 16 ? 1 : p.rows <= 32 || dim == 256 ? 2 : 4;
-    p.row_tiles = (p.rows + 16 * *nr - 1) / (16 * *nr);
+    p.many = p.rows > 32;
+    p.nr = p.many ? (p.rows <= 64 || dim == 256 ? 1 : 2) : (p.rows <= 16 ? 1 : 2);
+    const int32_t tile = (p.many ? 64 : 16) * p.nr;
+    p.row_tiles = (p.rows + tile - 1) / tile;
     const int64_t groups = (int64_t)p.row_tiles * c.heads * c.b;
     const int64_t most = ((int64_t)c.width * c.page + 127) / 128;
     int64_t splits = (512 + groups - 1) / groups;
@@ -67,8 +69,7 @@ static AttendPlan plan_attend(const AttendArgs &a, const CacheArgs &c, int dim, 
 
 size_t attend_workspace(const AttendArgs &a, const CacheArgs &c, int dim)
 {
-    int nr;
-    const AttendPlan p = plan_attend(a, c, dim, &nr);
+    const AttendPlan p = plan_attend(a, c, dim);
     if (p.splits == 1)
         return 0;
     return (size_t)p.splits * c.b * a.t * a.heads * (dim + 2) * sizeof(float);
@@ -89,11 +90,10 @@ static hipError_t launch_join(const AttendArgs &a, const AttendPlan &p, int64_t 
 
 hipError_t launch_attend(const AttendArgs &a, const CacheArgs &c, int bits, int dim, int type, void *ws, hipStream_t s)
 {
-    int nr;
-    AttendPlan p = plan_attend(a, c, dim, &nr);
+    AttendPlan p = plan_attend(a, c, dim);
     p.part = (float *)ws;
-    const hipError_t e = type == QNN_LM_BF16 ? launch_attend_bf16(a, c, p, bits, dim, nr, s)
-                                             : launch_attend_f16(a, c, p, bits, dim, nr, s);
+    const hipError_t e = type == QNN_LM_BF16 ? launch_attend_bf16(a, c, p, bits, dim, s)
+                                             : launch_attend_f16(a, c, p, bits, dim, s);
     if (e != hipSuccess || p.splits == 1)
         return e;
     const int64_t all = (int64_t)c.b * a.t * a.heads;
