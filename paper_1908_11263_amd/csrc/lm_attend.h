@@ -102,12 +102,44 @@ __device__ __forceinline__ void store_stats(const AttendArgs &a, const AttendPla
     }
 }
 
-// Largest exponent of the scales that lanes hold (-1000 where all are zero or
-// not finite).
+// o += V^T P^T for values v of which some are infinite or NaN, in a tile that
+// not every row sees whole: a position counts for the rows that see it (`see`:
+// 1 or 0) alone.  The finite values go through the product as ever; of the
+// others three products of ones count how many +infinity, -infinity and NaN a
+// row sees in a channel.
+template <class P>
+__device__ __forceinline__ f4 add_odd_values(s8_ v, typename P::V8 p, typename P::V8 see, f4 o)
+{
+    constexpr short inf = __is_same(P, Bf16) ? 0x7F80 : 0x7C00, one = __is_same(P, Bf16) ? 0x3F80 : 0x3C00;
+    s8_ fin, up, down, nan;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const short mag = v[e] & 0x7FFF;
+        fin[e] = mag < inf ? v[e] : 0;
+        up[e] = v[e] == inf ? one : 0;
+        down[e] = mag == inf && v[e] < 0 ? one : 0;
+        nan[e] = mag > inf ? one : 0;
+    }
+    const f4 zero = {0, 0, 0, 0};
+    using V = typename P::V8;
+    o = mfma16(__builtin_bit_cast(V, fin), p, o);
+    const f4 a = mfma16(__builtin_bit_cast(V, up), see, zero), b = mfma16(__builtin_bit_cast(V, down), see, zero),
+             c = mfma16(__builtin_bit_cast(V, nan), see, zero);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        o[i] += a[i] > 0.f ? INFINITY : 0.f;
+        o[i] += b[i] > 0.f ? -INFINITY : 0.f;
+        o[i] += c[i] > 0.f ? NAN : 0.f;
+    }
+    return o;
+}
+
+// Largest exponent of the scales that lanes hold, at least -120 (zeros and what
+// is not finite do not count).
 template <int LANES>
 __device__ __forceinline__ int scale_exponent(float v)
 {
-    int e = v > 0.f && v < INFINITY ? ilogbf(v) : -1000;
+    int e = v > 0.f && v < INFINITY ? max(ilogbf(v), -120) : -120;
 #pragma unroll
     for (int s = 1; s < LANES; s <<= 1)
         e = max(e, __shfl_xor(e, s, 64));

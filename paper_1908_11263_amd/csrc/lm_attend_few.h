@@ -331,24 +331,17 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                     o[n][d] = mfma16(vf, p[n], o[n][d]);
             }
         } else if constexpr (BITS == 16) {
-            // an infinite or NaN value that some row does not see: one
-            // position at a time, only where it is seen
 #pragma unroll
-            for (int n = 0; n < NR; ++n)
+            for (int n = 0; n < NR; ++n) {
+                typename N::V8 see;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    for (int from = 0; from < 4; ++from) {
-                        const float pe = __shfl((float)p[n][e], from * 16 + l16, 64);
-                        const float se = __shfl(s[n][e / 4][e % 4], from * 16 + l16, 64);
-                        const uint8_t *vr = vl + (16 * (e / 4) + 4 * from + e % 4) * S::kPitch;
-                        if (se == -INFINITY)
-                            continue;
+                for (int i = 0; i < 8; ++i)
+                    see[i] = (typename N::T)(s[n][i / 4][i % 4] != -INFINITY ? 1.f : 0.f);
 #pragma unroll
-                        for (int d = 0; d < ND; ++d)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                o[n][d][i] += pe * load1<N>(vr, d * 16 + 4 * kq + i);
-                    }
+                for (int d = 0; d < ND; ++d)
+                    o[n][d] = add_odd_values<N>(__builtin_bit_cast(s8_, value_frag<N, BITS, DIM>(vl, d, lane)), p[n], see,
+                                                o[n][d]);
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();

@@ -5,7 +5,7 @@
 // expanded once a workgroup: 64 positions at a time go from memory through
 // registers, where codes become 16-bit numbers, into local memory (two buffers,
 // one barrier a tile), from where the four waves read them for 16 NR rows each.
-// Loads run a tile ahead, page numbers two.
+// Loads run a tile ahead, or two where registers allow, page numbers one more.
 //
 // The maximum that probabilities are taken against is raised only where a score
 // is 2^8 above it: they stay below 2^8, their sum in fp32 loses nothing, and
@@ -31,14 +31,21 @@ struct ManyShape {
     static constexpr int kLanes = kBytes / 16;               // threads of a slot, 16 bytes each
     static constexpr int kLoads = KT * kLanes / 256;         // of a thread; 0: not every thread loads
     static constexpr int kMine = kLoads ? kLoads : 1;
+    static constexpr uint64_t kWhole = KT == 64 ? ~0ull : (1ull << KT) - 1;
     static constexpr int kPer = 128 / BITS;                  // numbers of a load
     static constexpr int kBuffer = 2 * KT * kRow + 2 * KT * 4;
     // workgroups a compute unit that the registers are shared out for: two,
     // but where the loads ahead (16-bit caches) or the outputs are too many
     static constexpr int groups(int nr) { return BITS == 16 && (nr == 2 || DIM == 256) ? 1 : 2; }
-    // place of piece c of row r: eight rows that read one piece, and four that
-    // read two neighbouring ones, find different banks
-    static __device__ __forceinline__ int place(int r, int c) { return c ^ (((r & 3) << 1) | ((r >> 2) & 1)); }
+    // Tiles that are loaded ahead, one set of registers each.
+    static constexpr int kAhead = BITS == 16 ? 1 : 2;
+    // place of piece c of row r: eight rows that read one piece, four that read
+    // two neighbouring ones, and eight lanes that write one or two rows' every
+    // second or fourth piece find different banks
+    static __device__ __forceinline__ int place(int r, int c)
+    {
+        return c ^ (((r & 3) << 1) | ((r >> 2) & 1)) ^ ((c >> 3) & 1);
+    }
 };
 
 // A load's numbers, from eight F on, to their row of local memory.
@@ -104,92 +111,127 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
             o[n][d] = (f4){0, 0, 0, 0};
     }
     const float qs = a.scale * 1.44269504088896f * (BITS == 4 ? 1.f / 16 : 1.f);
-    int vexp = -1000;
+    int vexp = -120;  // values' scales are taken as multiples of 2^vexp
+    float vscale = ldexpf(1.f, 120);
 
     const int32_t tiles = (end + KT - 1) / KT;
     const int32_t share = (tiles + pl.splits - 1) / pl.splits;
     const int32_t first = split * share, last = min(first + share, tiles);
 
-    // lane l looks position l of a tile up; page < 0: not there
-    auto look = [&](int32_t t) {
-        const int32_t pos = t * KT + lane;
-        int32_t page = -1;
-        if (t < last && lane < KT && pos < end) {
-            const int32_t pg = pl.shift >= 0 ? pos >> pl.shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
-            page = c.table[(int64_t)seq * c.width + pg];
-            if ((uint32_t)page >= (uint32_t)c.pages)
-                page = -1;
-        }
-        return page;
+    // Loads are never skipped: behind a branch that may skip one, a wait for an
+    // older load has to be a wait for all.  What is not there is read from a
+    // place that is (the last position's table entry, slot 0 of page 0), and
+    // cleared when it is staged.
+    //
+    // Page of a position as the table says.  Nothing is done with the number
+    // before load(): a comparison would wait for it here.
+    auto find = [&](int32_t t, int32_t r) {
+        const int32_t pos = max(min(t * KT + r, end - 1), 0);
+        const int32_t pg = pl.shift >= 0 ? pos >> pl.shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
+        return c.table[(int64_t)seq * c.width + pg];
     };
-    uint32_t kr[S::kMine][4], vr[S::kMine][4];
-    float ks = 0.f, vs = 0.f;
-    uint64_t valid = 0;
-    auto load = [&](int32_t t, int32_t page) {
-        const int32_t pos = t * KT + lane;
-        const int32_t slot =
-            pl.shift >= 0 ? pos & ((1 << pl.shift) - 1) : (int32_t)((uint32_t)pos % (uint32_t)c.page);
-        valid = __ballot(page >= 0);
+    auto in_cache = [&](int32_t t, int32_t r, int32_t page) {
+        return t < last && r < KT && t * KT + r < end && (uint32_t)page < (uint32_t)c.pages;
+    };
+    auto slot_of = [&](int32_t pos) {
+        return pl.shift >= 0 ? pos & ((1 << pl.shift) - 1) : (int32_t)((uint32_t)pos % (uint32_t)c.page);
+    };
+    // A tile's pages: of position `lane`, and of the positions that this thread loads
+    struct Pages {
+        int32_t mine, of[S::kMine];
+    };
+    auto look = [&](int32_t t) {
+        Pages p;
+        p.mine = find(t, lane);
+#pragma unroll
+        for (int i = 0; i < S::kMine; ++i)
+            p.of[i] = find(t, (i * 256 + threadIdx.x) / S::kLanes % KT);
+        return p;
+    };
+    struct Ahead {
+        uint32_t k[S::kMine][4], v[S::kMine][4];
+        float ks, vs;    // scales of position `lane`
+        uint64_t valid;  // positions that are in the cache
+    };
+    const uint8_t *kb = c.k + head * c.k_head, *vb0 = c.v + head * c.v_head;
+    auto load = [&](Ahead &h, int32_t t, const Pages &p) {
+        const bool there = in_cache(t, lane, p.mine);
+        h.valid = __ballot(there);
         if constexpr (BITS != 16) {
-            ks = vs = 0.f;
-            if (page >= 0) {
-                const int64_t at = ((int64_t)page * c.heads + head) * c.page + slot;
-                ks = c.k_scale[at];
-                vs = c.v_scale[at];
-            }
+            const int64_t at =
+                there ? ((int64_t)p.mine * c.heads + head) * c.page + slot_of(t * KT + lane) : 0;
+            h.ks = c.k_scale[at];
+            h.vs = c.v_scale[at];
         }
 #pragma unroll
         for (int i = 0; i < S::kMine; ++i) {
-            const int e = i * 256 + threadIdx.x, r = e / S::kLanes, piece = e % S::kLanes;
-            const int32_t pg = __shfl(page, r & 63, 64), sl = __shfl(slot, r & 63, 64);
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-                kr[i][w] = vr[i][w] = 0;
-            if (pg >= 0 && r < KT) {
-                load_words<4>(c.k + pg * c.k_page + head * c.k_head + sl * c.k_slot + piece * 16, kr[i]);
-                load_words<4>(c.v + pg * c.v_page + head * c.v_head + sl * c.v_slot + piece * 16, vr[i]);
-            }
+            const int e = i * 256 + threadIdx.x, r = e / S::kLanes % KT, piece = e % S::kLanes;
+            const bool here = in_cache(t, r, p.of[i]);
+            const int32_t pg = here ? p.of[i] : 0, sl = here ? slot_of(t * KT + r) : 0;
+            load_words<4>(kb + pg * c.k_page + sl * c.k_slot + piece * 16, h.k[i]);
+            load_words<4>(vb0 + pg * c.v_page + sl * c.v_slot + piece * 16, h.v[i]);
         }
     };
     // registers to local memory, codes as numbers
-    auto stage = [&](uint8_t *buf) {
+    auto stage = [&](Ahead &h, uint8_t *buf) {
+        if (h.valid != S::kWhole) {
+            // (keys that are not there are masked, values have to be zero)
+#pragma unroll
+            for (int i = 0; i < S::kMine; ++i)
+                if (!((h.valid >> ((i * 256 + threadIdx.x) / S::kLanes % KT)) & 1))
+                    h.v[i][0] = h.v[i][1] = h.v[i][2] = h.v[i][3] = 0;
+        }
 #pragma unroll
         for (int i = 0; i < S::kMine; ++i) {
             const int e = i * 256 + threadIdx.x, r = e / S::kLanes, piece = e % S::kLanes;
             if (S::kLoads == 0 && r >= KT)
                 continue;
             uint8_t *kp = buf + r * S::kRow, *vp = kp + KT * S::kRow;
-            stage_pieces<N, P, BITS, DIM, 0>(kp, vp, kr[i], vr[i], r, piece);
+            stage_pieces<N, P, BITS, DIM, 0>(kp, vp, h.k[i], h.v[i], r, piece);
         }
         if constexpr (BITS != 16) {
             float *sc = (float *)(buf + 2 * KT * S::kRow);
             if (wave == 0 && lane < KT) {
-                sc[lane] = ks * qs;
-                sc[KT + lane] = ldexpf(vs * (BITS == 4 ? 1.f / 16 : 1.f), -vexp);
+                sc[lane] = h.ks * qs;
+                sc[KT + lane] = h.vs * (BITS == 4 ? vscale / 16 : vscale);
             }
         }
     };
 
-    load(first, look(first));
-    int32_t page = look(first + 1);
-    for (int32_t t = first; t < last; ++t) {
+    Ahead ahead[S::kAhead];
+    Pages early[S::kAhead];
+#pragma unroll
+    for (int i = 0; i < S::kAhead; ++i)
+        early[i] = look(first + i);
+    Pages page = look(first + S::kAhead);
+#pragma unroll
+    for (int i = 0; i < S::kAhead; ++i)
+        load(ahead[i], first + i, early[i]);
+    auto step = [&](Ahead &h, int32_t t) {
         uint8_t *buf = lds + ((t - first) & 1) * S::kBuffer;
-        const uint64_t there = valid;
+        const uint64_t there = h.valid;
+        if (BITS != 16 && there != S::kWhole && !((there >> lane) & 1))
+            h.ks = h.vs = 0.f;
+        const float vsmine = BITS == 16 ? 0.f : h.vs;
         if constexpr (BITS != 16) {
-            const int e = scale_exponent<64>(vs);
-            if (e > vexp) {
-                const float f = ldexpf(1.f, max(vexp - e, -300));
+            // (scales that are not finite stay so)
+            if (__any(h.vs * vscale >= 2.f && h.vs < INFINITY)) {
+                const int e = scale_exponent<64>(h.vs);
+                const float f = ldexpf(1.f, vexp - e);
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
                         o[n][d] *= f;
                 vexp = e;
+                vscale = ldexpf(1.f, -e);
             }
         }
-        stage(buf);
-        load(t + 1, page);
-        page = look(t + 2);
+        stage(h, buf);
+        // (the page numbers first: loads come back in order, and these are wanted before the tile's)
+        const Pages later = look(t + S::kAhead + 1);
+        load(h, t + S::kAhead, page);
+        page = later;
         // local memory is written; the loads ahead stay in flight
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -198,19 +240,24 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
         const uint8_t *vb = buf + KT * S::kRow;
         const float *sc = (const float *)(buf + 2 * KT * S::kRow);
         f4 s[NR][NU];
+        // (the products of a row's sixteens do not wait for each other)
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const int r = 16 * u + l16;
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
             for (int n = 0; n < NR; ++n)
                 s[n][u] = (f4){0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NK; ++i) {
+        for (int i = 0; i < NK; ++i)
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const int r = 16 * u + l16;
                 const typename N::V8 kf = *(const typename N::V8 *)(buf + r * S::kRow + S::place(r, 4 * i + kq) * 16);
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
                     s[n][u] = mfma16(kf, q[n][i], s[n][u]);
             }
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
             f4 ku = {qs, qs, qs, qs};
             if constexpr (BITS != 16)
                 ku = *(const f4 *)(sc + 16 * u + 4 * kq);
@@ -219,7 +266,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                 s[n][u] *= ku;
         }
         const int32_t p0 = t * KT;
-        const bool whole = there == (KT == 64 ? ~0ull : (1ull << KT) - 1) && p0 + KT <= sq.len;
+        const bool whole = there == S::kWhole && p0 + KT <= sq.len;
         if (!whole) {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
@@ -232,6 +279,9 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                         s[n][u][i] = (see >> (16 * u + i)) & 1 ? s[n][u][i] : -INFINITY;
             }
         }
+        // a scale that is not finite, and that some row does not see: what it
+        // holds has no influence there
+        const bool bad = BITS != 16 && !whole && __any(!(fabsf(vsmine) < INFINITY));
         typename P::V8 p[NR][NU / 2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -269,8 +319,14 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                         const f4 vu = *(const f4 *)(sc + KT + 32 * h + 16 * u + 4 * kq);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            // (a select: what an unseen position's scale holds has no influence)
-                            e[4 * u + i] = whole || s[n][2 * h + u][i] != -INFINITY ? e[4 * u + i] * vu[i] : 0.f;
+                            e[4 * u + i] *= vu[i];
+                    }
+                    if (bad) {
+                        asm volatile("");  // (a branch, not a select in every tile)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (s[n][2 * h + i / 4][i % 4] == -INFINITY)
+                                e[i] = 0.f;
                     }
                 }
                 const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
@@ -290,46 +346,47 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                 odd = __any(odd);
             }
         }
+        auto values = [&](int h, int d) {
+            const int r = 32 * h + 4 * kq + (l16 >> 2);
+            // (rows r and r + 16 have their pieces in the same places)
+            const uint8_t *vp = vb + r * S::kRow + S::place(r, 2 * d + ((l16 >> 1) & 1)) * 16 + (l16 & 1) * 8;
+            const s4_ x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)vp);
+            const s4_ y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(vp + 16 * S::kRow));
+            return (s8_){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        };
         if (!odd) {
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+            for (int h = 0; h < NU / 2; ++h)
 #pragma unroll
-                for (int h = 0; h < NU / 2; ++h) {
-                    const int r = 32 * h + 4 * kq + (l16 >> 2);
-                    // (rows r and r + 16 have their pieces in the same places)
-                    const uint8_t *vp = vb + r * S::kRow + S::place(r, 2 * d + ((l16 >> 1) & 1)) * 16 + (l16 & 1) * 8;
-                    const s4_ x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)vp);
-                    const s4_ y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(vp + 16 * S::kRow));
-                    const s8_ z = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                for (int d = 0; d < ND; ++d) {
+                    const s8_ z = values(h, d);
 #pragma unroll
                     for (int n = 0; n < NR; ++n)
                         o[n][d] = mfma16(__builtin_bit_cast(typename P::V8, z), p[n][h], o[n][d]);
                 }
         } else if constexpr (BITS == 16) {
-            // an infinite or NaN value that some row does not see: one position
-            // at a time, only where it is seen
 #pragma unroll
-            for (int n = 0; n < NR; ++n)
+            for (int h = 0; h < NU / 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4 * NU; ++e)
-                    for (int from = 0; from < 4; ++from) {
-                        const float pe = __shfl((float)p[n][e / 8][e % 8], from * 16 + l16, 64);
-                        const float se = __shfl(s[n][e / 4][e % 4], from * 16 + l16, 64);
-                        if (se == -INFINITY)
-                            continue;
-                        const int r = 16 * (e / 4) + 4 * from + e % 4;
+                for (int n = 0; n < NR; ++n) {
+                    typename P::V8 see;
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) {
-                            const uint8_t *vp = vb + r * S::kRow + S::place(r, 2 * d + (kq >> 1)) * 16 + (kq & 1) * 8;
+                    for (int i = 0; i < 8; ++i)
+                        see[i] = (typename P::T)(s[n][2 * h + i / 4][i % 4] != -INFINITY ? 1.f : 0.f);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                o[n][d][i] += pe * load1<N>(vp, i);
-                        }
-                    }
+                    for (int d = 0; d < ND; ++d)
+                        o[n][d] = add_odd_values<P>(values(h, d), p[n][h], see, o[n][d]);
+                }
         }
+    };
+    for (int32_t t = first; t < last; t += S::kAhead) {
+        step(ahead[0], t);
+        if constexpr (S::kAhead == 2)
+            if (t + 1 < last)
+                step(ahead[1], t + 1);
     }
     const int64_t all = (int64_t)c.b * a.t * a.heads;
-    const float f = BITS == 16 || vexp == -1000 ? 1.f : ldexpf(1.f, vexp);
+    const float f = BITS == 16 ? 1.f : ldexpf(1.f, vexp);
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         l[n] += __shfl_xor(l[n], 16, 64);
