@@ -17,6 +17,15 @@
 //         A = V^T comes from local memory by the transposing reads.
 // Codes enter the products as they are (exact); a key's scale multiplies its
 // scores, a value's scale its probabilities.
+//
+// The reference m that probabilities 2^(score - m) are taken against is not the
+// maximum but kAbove below it, and is raised only where a score is kSlack above
+// what it was set for: most tiles neither exchange maxima between lanes nor
+// rescale.  Probabilities stay below 2^(kAbove + kSlack) = 2^14, so that f16
+// holds them, and keep all its bits down to 2^-24 of the largest; sums are fp32.
+// Values of a packed cache are multiplied as f16 whatever the queries' type
+// (codes are exact there, and probabilities keep 11 bits): their scales are
+// taken relative to a power of two, the largest so far, so that they stay below 2.
 #pragma once
 
 #include "lm_cache.h"
@@ -28,6 +37,8 @@ typedef short s8_ __attribute__((ext_vector_type(8)));
 typedef int i2_ __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s4_ lds_s4;
 typedef __attribute__((address_space(3))) i2_ lds_i2;
+
+constexpr float kAbove = 10.f, kSlack = 4.f;
 
 struct AttendPlan {
     int32_t g;          // query heads of a cache head

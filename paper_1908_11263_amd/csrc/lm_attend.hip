@@ -40,8 +40,9 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part, void *out,
         lse[row] = m == -INFINITY ? -INFINITY : 0.693147180559945f * (m + log2f(l));
 }
 
-// Rows a workgroup and pieces of the positions.  Up to 32 rows go to the kernel
-// whose waves share out the positions.  Positions are split until there are two
+// Rows a workgroup and pieces of the positions.  Up to 32 rows (16 of 256
+// channels, whose outputs fill the registers) go to the kernel whose waves share
+// out the positions.  Positions are split until there are two
 // workgroups for each of the 256 compute units, in pieces of at least 128
 // positions.  Lengths live on the device: the plan goes by what the table can
 // reach, the kernels share out the positions that there are.
@@ -50,7 +51,7 @@ static AttendPlan plan_attend(const AttendArgs &a, const CacheArgs &c, int dim)
     AttendPlan p;
     p.g = a.heads / c.heads;
     p.rows = a.t * p.g;
-    p.many = p.rows > 32;
+    p.many = p.rows > (dim == 256 ? 16 : 32);
     p.nr = p.many ? (p.rows <= 64 || dim == 256 ? 1 : 2) : (p.rows <= 16 ? 1 : 2);
     const int32_t tile = (p.many ? 64 : 16) * p.nr;
     p.row_tiles = (p.rows + tile - 1) / tile;

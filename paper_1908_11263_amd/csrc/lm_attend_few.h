@@ -2,6 +2,8 @@
 // workgroup share out the positions.
 #pragma once
 
+#include <type_traits>
+
 #include "lm_attend.h"
 
 namespace qnn_lm {
@@ -35,56 +37,65 @@ struct KvTile {
     float ks, vs;     // of position lane % 32
     uint32_t valid;   // positions that are in the cache and before the end
 
-    __device__ __forceinline__ void load(const CacheArgs &c, int shift, int32_t seq, int32_t head, int32_t p0,
+    // Page of position lane % 32 as the table says; looked at in load(), a tile
+    // later (loads come back in order: a comparison here would wait for all).
+    static __device__ __forceinline__ int32_t look(const CacheArgs &c, int shift, int32_t seq, int32_t p0, int32_t end,
+                                                   int lane)
+    {
+        const int32_t pos = max(min(p0 + (lane & 31), end - 1), 0);
+        const int32_t pg = shift >= 0 ? pos >> shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
+        return c.table[(int64_t)seq * c.width + pg];
+    }
+
+    // Loads are never skipped (behind a branch that may skip one, a wait for an
+    // older load has to be a wait for all): what is not there is read from slot
+    // 0 of page 0, and masked or cleared later.
+    __device__ __forceinline__ void load(const CacheArgs &c, int shift, int32_t page, int32_t head, int32_t p0,
                                          int32_t end, int lane)
     {
-        const int l32 = lane & 31;
-        // lane l % 32 looks its position up; the others take it from there
-        Slot s = {-1, 0};
-        const int32_t pos = p0 + l32;
-        if (pos < end) {
-            const int32_t pg = shift >= 0 ? pos >> shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
-            const int32_t page = c.table[(int64_t)seq * c.width + pg];
-            if ((uint32_t)page < (uint32_t)c.pages) {
-                s.page = page;
-                s.slot = pos - pg * c.page;
-            }
-        }
-        valid = (uint32_t)__ballot(s.page >= 0);
+        const int32_t pos = p0 + (lane & 31);
+        const bool there = pos < end && (uint32_t)page < (uint32_t)c.pages;
+        valid = (uint32_t)__ballot(there);
+        int32_t slot = shift >= 0 ? pos & ((1 << shift) - 1) : (int32_t)((uint32_t)pos % (uint32_t)c.page);
+        page = there ? page : 0;
+        slot = there ? slot : 0;
         if constexpr (BITS != 16) {
-            ks = vs = 0.f;
-            if (s.page >= 0) {
-                const int64_t at = scale_at(c, s, head);
-                ks = c.k_scale[at];
-                vs = c.v_scale[at];
-            }
+            const int64_t at = ((int64_t)page * c.heads + head) * c.page + slot;
+            ks = c.k_scale[at];
+            vs = c.v_scale[at];
         }
+        // lane l % 32 has looked its position up; the others take it from there
         const int l16 = lane & 15, kq = lane >> 4;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int32_t page = __shfl(s.page, 16 * u + l16, 64), slot = __shfl(s.slot, 16 * u + l16, 64);
-            const uint8_t *p = c.k + page * c.k_page + head * c.k_head + slot * c.k_slot;
+            const int32_t pg = __shfl(page, 16 * u + l16, 64), sl = __shfl(slot, 16 * u + l16, 64);
+            const uint8_t *p = c.k + pg * c.k_page + head * c.k_head + sl * c.k_slot;
 #pragma unroll
-            for (int i = 0; i < S::kLoads; ++i) {
-#pragma unroll
-                for (uint32_t &w : k[u][i])
-                    w = 0;
-                if (page >= 0)
-                    load_words<S::kWords>(p + (i * 4 + kq) * (S::kWords * 4), k[u][i]);
-            }
+            for (int i = 0; i < S::kLoads; ++i)
+                load_words<S::kWords>(p + (i * 4 + kq) * (S::kWords * 4), k[u][i]);
         }
 #pragma unroll
         for (int i = 0; i < S::kVLoads; ++i) {
             const int row = i * (64 / S::kVLanes) + lane / S::kVLanes;
-            const int32_t page = __shfl(s.page, row, 64), slot = __shfl(s.slot, row, 64);
-#pragma unroll
-            for (uint32_t &w : v[i])
-                w = 0;
-            if (page >= 0)
-                load_words<S::kVWords>(c.v + page * c.v_page + head * c.v_head + slot * c.v_slot +
-                                           (lane % S::kVLanes) * S::kVLane,
-                                       v[i]);
+            const int32_t pg = __shfl(page, row, 64), sl = __shfl(slot, row, 64);
+            load_words<S::kVWords>(c.v + pg * c.v_page + head * c.v_head + sl * c.v_slot + (lane % S::kVLanes) * S::kVLane,
+                                   v[i]);
         }
+    }
+
+    // Clears the values and scales of positions that are not there (keys are masked).
+    __device__ __forceinline__ void clear(int lane)
+    {
+        if (valid == 0xFFFFFFFFu)
+            return;
+        if (BITS != 16 && !((valid >> (lane & 31)) & 1))
+            ks = vs = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::kVLoads; ++i)
+            if (!((valid >> (i * (64 / S::kVLanes) + lane / S::kVLanes)) & 1))
+#pragma unroll
+                for (uint32_t &w : v[i])
+                    w = 0;
     }
 
     // s[n][u] += the I-th and later products of half u's keys with the queries
@@ -162,20 +173,16 @@ template <class N, int BITS, int DIM, int NR>
 __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, AttendPlan pl)
 {
     using S = KvShape<BITS, DIM>;
+    using P = std::conditional_t<BITS == 16, N, F16>;  // type of the second product
     constexpr int ND = DIM / 16, NK = DIM / 32;
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t split = blockIdx.x % pl.splits, tile = blockIdx.x / pl.splits;
     const int32_t head = blockIdx.y, seq = blockIdx.z;
-    const int32_t len = max(a.lens[seq], 0);
-    const int32_t count = a.counts ? min(max(a.counts[seq], 0), a.t) : a.t;
+    const AttendSeq sq(a, seq);
     const int32_t row0 = tile * 16 * NR;
-    // positions that a row of this tile can see end here
-    const int32_t last_draft = min(count, (min(row0 + 16 * NR, pl.rows) - 1) / pl.g + 1);
-    const int32_t seen = row0 / pl.g >= count ? 0 : a.mask ? count : last_draft;
-    const int64_t reach = (int64_t)c.width * c.page;
-    const int32_t end = seen ? (int32_t)min((int64_t)len + seen, reach) : 0;
+    const int32_t end = sq.end(a, c, pl, row0, 16 * NR);
 
     // this lane's rows: queries and draft numbers
     typename N::V8 q[NR][NK];
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
     for (int n = 0; n < NR; ++n) {
         const int32_t row = row0 + n * 16 + l16;
         draft[n] = row < pl.rows ? row / pl.g : -1;
-        const bool live = draft[n] >= 0 && draft[n] < count;
+        const bool live = draft[n] >= 0 && draft[n] < sq.count;
         const typename N::T *p = (const typename N::T *)a.q + seq * a.q_b + max(draft[n], 0) * a.q_t +
                                  (head * pl.g + (live ? row - draft[n] * pl.g : 0)) * a.q_h;
         if (!live)
@@ -210,46 +217,46 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             o[n][d] = (f4){0, 0, 0, 0};
     }
     const float qs = a.scale * 1.44269504088896f * (BITS == 4 ? 1.f / 16 : 1.f);  // scores in powers of two
-    // f16 only: values' scales are taken relative to 2^vexp, so that the
-    // probabilities that they multiply stay normal numbers
-    int vexp = -1000;
+    int vexp = -120;  // values' scales are taken as multiples of 2^vexp
+    float vscale = ldexpf(1.f, 120);
     uint8_t *vl = lds + wave * S::kWaveLds;
     float *scales = (float *)(vl + kAttendTile * S::kPitch);
 
     const int32_t tiles = (end + kAttendTile - 1) / kAttendTile;
     const int32_t share = (tiles + pl.splits - 1) / pl.splits;
-    const int32_t last = min((split + 1) * share, tiles);
-    int32_t at = split * share + wave;
-    KvTile<BITS, DIM> cur, next;
-    if (at < last)
-        cur.load(c, pl.shift, seq, head, at * kAttendTile, end, lane);
-    for (; at < last; at += 4) {
-        if (at + 4 < last)
-            next.load(c, pl.shift, seq, head, (at + 4) * kAttendTile, end, lane);
+    const int32_t first = split * share + wave, last = min((split + 1) * share, tiles);
+    using Tile = KvTile<BITS, DIM>;
+    auto look = [&](int32_t t) { return Tile::look(c, pl.shift, seq, t * kAttendTile, end, lane); };
+    // (tiles past the last are loaded too, from slot 0 of page 0, and not used)
+    auto load = [&](Tile &h, int32_t t, int32_t page) {
+        h.load(c, pl.shift, page, head, t * kAttendTile, t < last ? end : 0, lane);
+    };
+    Tile ahead[2];
+    const int32_t early[2] = {look(first), look(first + 4)};
+    int32_t page = look(first + 8);
+    load(ahead[0], first, early[0]);
+    load(ahead[1], first + 4, early[1]);
+    auto step = [&](Tile &cur, int32_t at) {
         const int32_t p0 = at * kAttendTile;
+        cur.clear(lane);
         cur.stage(vl, lane);
+        const uint32_t there = cur.valid;
         if constexpr (BITS != 16) {
-            float vs = cur.vs * (BITS == 4 ? 1.f / 16 : 1.f);
-            if constexpr (__is_same(N, F16)) {
-                // (scales that are not finite stay so)
-                int e = vs > 0.f && vs < INFINITY ? ilogbf(vs) : -1000;
+            // (scales that are not finite stay so)
+            if (__any(cur.vs * vscale >= 2.f && cur.vs < INFINITY)) {
+                const int e = scale_exponent<32>(cur.vs);
+                const float f = ldexpf(1.f, vexp - e);
 #pragma unroll
-                for (int s = 1; s < 32; s <<= 1)
-                    e = max(e, __shfl_xor(e, s, 64));
-                if (e > vexp) {
-                    const float f = ldexpf(1.f, max(vexp - e, -300));
+                for (int n = 0; n < NR; ++n)
 #pragma unroll
-                    for (int n = 0; n < NR; ++n)
-#pragma unroll
-                        for (int d = 0; d < ND; ++d)
-                            o[n][d] *= f;
-                    vexp = e;
-                }
-                vs = ldexpf(vs, -vexp);
+                    for (int d = 0; d < ND; ++d)
+                        o[n][d] *= f;
+                vexp = e;
+                vscale = ldexpf(1.f, -e);
             }
             if (lane < 32) {
                 scales[lane] = cur.ks * qs;
-                scales[32 + lane] = vs;
+                scales[32 + lane] = cur.vs * vscale;
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -276,11 +283,19 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             for (int n = 0; n < NR; ++n)
                 s[n][u] *= ks[u];
         }
-        const bool whole = cur.valid == 0xFFFFFFFFu && p0 + kAttendTile <= len;
+        const bool whole = there == 0xFFFFFFFFu && p0 + kAttendTile <= sq.len;
+        const bool bad = BITS != 16 && !whole && __any(!(fabsf(cur.vs) < INFINITY));
+        bool odd = false;
+        if constexpr (BITS == 16)
+            odd = !whole && cur.template odd_values<N>();
+        // the tile's registers are free: two tiles on, into the same ones
+        const int32_t later = look(at + 12);
+        load(cur, at + 8, page);
+        page = later;
         if (!whole) {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                uint32_t see = draft[n] < 0 ? 0 : (uint32_t)seen_bits(a, seq, draft[n], p0, len) & cur.valid;
+                uint32_t see = draft[n] < 0 ? 0 : (uint32_t)seen_bits(a, seq, draft[n], p0, sq.len) & there;
                 see >>= 4 * kq;
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
@@ -289,15 +304,15 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                         s[n][u][i] = (see >> (16 * u + i)) & 1 ? s[n][u][i] : -INFINITY;
             }
         }
-        typename N::V8 p[NR];
+        typename P::V8 p[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
                               fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            if (__any(top > m[n])) {
-                const float mn = fmaxf(m[n], top);
+            if (__any(top > m[n] + kAbove + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float mn = fmaxf(m[n], top - kAbove);
                 // (rows that have seen nothing: 2^(-inf) = 0, of zeros)
                 const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - mn);
                 m[n] = mn;
@@ -312,20 +327,23 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             for (int i = 0; i < 8; ++i) {
                 e[i] = __builtin_amdgcn_exp2f(s[n][i / 4][i % 4] - mm);
                 l[n] += e[i];
-                // (a select: what an unseen position's scale holds has no influence)
                 if constexpr (BITS != 16)
-                    e[i] = whole || s[n][i / 4][i % 4] != -INFINITY ? e[i] * vs[i / 4][i % 4] : 0.f;
+                    e[i] *= vs[i / 4][i % 4];
             }
-            const u4 r = {pack2<N>(e[0], e[1]), pack2<N>(e[2], e[3]), pack2<N>(e[4], e[5]), pack2<N>(e[6], e[7])};
-            p[n] = __builtin_bit_cast(typename N::V8, r);
+            if (bad) {
+                asm volatile("");  // (a branch, not a select in every tile)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (s[n][i / 4][i % 4] == -INFINITY)
+                        e[i] = 0.f;  // what an unseen position's scale holds has no influence
+            }
+            const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
+            p[n] = __builtin_bit_cast(typename P::V8, r);
         }
-        bool odd = false;
-        if constexpr (BITS == 16)
-            odd = !whole && cur.template odd_values<N>();
         if (!odd) {
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
-                const typename N::V8 vf = value_frag<N, BITS, DIM>(vl, d, lane);
+                const typename P::V8 vf = value_frag<P, BITS, DIM>(vl, d, lane);
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
                     o[n][d] = mfma16(vf, p[n], o[n][d]);
@@ -345,7 +363,11 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        cur = next;
+    };
+    for (int32_t at = first; at < last; at += 8) {
+        step(ahead[0], at);
+        if (at + 4 < last)
+            step(ahead[1], at + 4);
     }
     // join the four waves, sixteen rows at a time
     constexpr int OP = DIM + 4;  // pitch in floats
@@ -367,14 +389,12 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         for (int w = 1; w < 4; ++w)
             top = fmaxf(top, jm[w * 16 + l16]);
         float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - top);
-        // (a wave that saw no scale has no outputs either)
-        if (BITS != 16 && __is_same(N, F16))
-            f = vexp == -1000 ? 0.f : ldexpf(f, vexp);
-        if (m[n] == -INFINITY)
-            f = 0.f;
+        if constexpr (BITS != 16)
+            f = ldexpf(f, BITS == 4 ? vexp - 4 : vexp);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
-            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = o[n][d] * f;
+            // (a row that has seen nothing may hold anything)
+            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = m[n] == -INFINITY ? (f4){0, 0, 0, 0} : o[n][d] * f;
         __syncthreads();
         // 16 threads a row
         const int r = threadIdx.x >> 4, e0 = threadIdx.x & 15;

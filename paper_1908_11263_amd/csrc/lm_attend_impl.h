@@ -47,7 +47,10 @@ hipError_t launch_attend_dim(const AttendArgs &a, const CacheArgs &c, const Atte
                 return launch_many<N, BITS, DIM, 2>(a, c, p, s);
         return launch_many<N, BITS, DIM, 1>(a, c, p, s);
     }
-    return p.nr == 1 ? launch_few<N, BITS, DIM, 1>(a, c, p, s) : launch_few<N, BITS, DIM, 2>(a, c, p, s);
+    if constexpr (DIM < 256)
+        if (p.nr == 2)
+            return launch_few<N, BITS, DIM, 2>(a, c, p, s);
+    return launch_few<N, BITS, DIM, 1>(a, c, p, s);
 }
 
 template <class N, int BITS>

@@ -6,14 +6,6 @@
 // registers, where codes become 16-bit numbers, into local memory (two buffers,
 // one barrier a tile), from where the four waves read them for 16 NR rows each.
 // Loads run a tile ahead, or two where registers allow, page numbers one more.
-//
-// The maximum that probabilities are taken against is raised only where a score
-// is 2^8 above it: they stay below 2^8, their sum in fp32 loses nothing, and
-// most tiles neither exchange maxima between lanes nor rescale.
-//
-// Values of a packed cache are multiplied as f16 whatever the queries' type
-// (codes are exact, and probabilities keep 11 bits): value scales are taken
-// relative to the largest so far, a power of two, so that they stay in range.
 #pragma once
 
 #include <type_traits>
@@ -193,7 +185,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
             float *sc = (float *)(buf + 2 * KT * S::kRow);
             if (wave == 0 && lane < KT) {
                 sc[lane] = h.ks * qs;
-                sc[KT + lane] = h.vs * (BITS == 4 ? vscale / 16 : vscale);
+                sc[KT + lane] = h.vs * vscale;
             }
         }
     };
@@ -291,10 +283,10 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
 #pragma unroll
                 for (int i = 0; i < 4; i += 2)
                     top = fmaxf(fmaxf(s[n][u][i], s[n][u][i + 1]), top);
-            if (__any(top > m[n] + 8.f)) {
+            if (__any(top > m[n] + kAbove + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float mn = fmaxf(m[n], top);
+                const float mn = fmaxf(m[n], top - kAbove);
                 // (rows that have seen nothing keep their zeros)
                 const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - mn);
                 m[n] = mn;
@@ -386,7 +378,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                 step(ahead[1], t + 1);
     }
     const int64_t all = (int64_t)c.b * a.t * a.heads;
-    const float f = BITS == 16 ? 1.f : ldexpf(1.f, vexp);
+    const float f = BITS == 16 ? 1.f : ldexpf(1.f, BITS == 4 ? vexp - 4 : vexp);
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         l[n] += __shfl_xor(l[n], 16, 64);
