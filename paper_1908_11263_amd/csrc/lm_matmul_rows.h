@@ -25,35 +25,46 @@ struct RowsTile {
     typename N::V8 x[NC][NF];
     float scale[WR];
 
+    // (Never skipped: behind a branch that may skip a load, a wait for an older
+    // one has to be a wait for all.  Pieces past k are read from the row's start
+    // and cleared in add().)
     __device__ __forceinline__ void load(const MatmulArgs &a, const uint8_t *const (&wp)[WR],
                                          const typename N::T *const (&xp)[NC], const float *const (&sp)[WR],
                                          int32_t k0, int kq)
     {
-        const int32_t k = k0 + kq * 8 * NF;  // this lane's piece
-        const bool in = k < a.k;
+        int32_t k = k0 + kq * 8 * NF;  // this lane's piece
+        k = k < a.k ? k : 0;
+#pragma unroll
+        for (int r = 0; r < WR; ++r) {
+            load_raw<kRaw<BITS, NF>>(wp[r] + (int64_t)k * BITS / 8, w[r]);
+            if constexpr (BITS != 16)
+                scale[r] = sp[r][a.groups > 1 ? k0 >> __builtin_ctz(a.group) : 0];
+        }
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                u4 v = {0, 0, 0, 0};
-                if (in && xp[c])
-                    v = *(const u4 *)(xp[c] + k + 8 * f);
-                x[c][f] = __builtin_bit_cast(typename N::V8, v);
-            }
-#pragma unroll
-        for (int r = 0; r < WR; ++r) {
-#pragma unroll
-            for (uint32_t &v : w[r])
-                v = 0;
-            if (in)
-                load_raw<kRaw<BITS, NF>>(wp[r] + (int64_t)k * BITS / 8, w[r]);
-            if constexpr (BITS != 16)
-                scale[r] = a.groups > 1 ? sp[r][k0 / a.group] : 1.f;
-        }
+            for (int f = 0; f < NF; ++f)
+                x[c][f] = *(const typename N::V8 *)(xp[c] + k + 8 * f);
     }
 
-    __device__ __forceinline__ void add(f4 (&acc)[WR][NC], bool grouped) const
+    __device__ __forceinline__ void add(f4 (&acc)[WR][NC], const MatmulArgs &a, int32_t k0, int kq)
     {
+        const bool grouped = BITS != 16 && a.groups > 1;
+        if (k0 + kStep > a.k && k0 + kq * 8 * NF >= a.k) {
+            // (a code is finite whatever its bits, a 16-bit weight need not be)
+            const u4 zero = {0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+                    x[c][f] = __builtin_bit_cast(typename N::V8, zero);
+            if constexpr (BITS == 16)
+#pragma unroll
+                for (int r = 0; r < WR; ++r)
+#pragma unroll
+                    for (uint32_t &v : w[r])
+                        v = 0;
+        }
 #pragma unroll
         for (int r = 0; r < WR; ++r) {
             f4 part[NC];
@@ -84,6 +95,7 @@ template <class N, int BITS, int NF, int WR, int NC, bool GATED, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
 {
     using Tile = RowsTile<N, BITS, NF, WR, NC, GATED>;
+    constexpr int AHEAD = NC == 1 ? 4 : 2;
     extern __shared__ f4 part[];  // [wave][WR][NC][64]
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -102,8 +114,8 @@ __global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int32_t r = r0 + c * 16 + l16;
-        xp[c] = r < a.r ? (const typename N::T *)a.x + r * a.x_pitch : nullptr;
+        const int32_t r = min(r0 + c * 16 + l16, a.r - 1);
+        xp[c] = (const typename N::T *)a.x + r * a.x_pitch;
     }
     f4 acc[WR][NC];
 #pragma unroll
@@ -115,16 +127,23 @@ __global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
     const int32_t steps = (a.k + Tile::kStep - 1) / Tile::kStep;
     const int32_t share = (steps + WAVES - 1) / WAVES;
     const int32_t first = min(wave * share, steps), last = min(first + share, steps);
-    const bool grouped = BITS != 16 && a.groups > 1;
-    Tile cur, next;
-    if (first < last)
-        cur.load(a, wp, xp, sp, first * Tile::kStep, kq);
-    for (int32_t s = first; s < last; ++s) {
-        if (s + 1 < last)
-            next.load(a, wp, xp, sp, (s + 1) * Tile::kStep, kq);
-        cur.add(acc, grouped);
-        cur = next;
-    }
+    // AHEAD steps are in flight, each in registers of its own
+    Tile t[AHEAD];
+    auto load = [&](Tile &tile, int32_t s) { tile.load(a, wp, xp, sp, max(min(s, last - 1), 0) * Tile::kStep, kq); };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        load(t[i], first + i);
+    int32_t s = first;
+    for (; last - s > AHEAD; s += AHEAD)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            t[i].add(acc, a, (s + i) * Tile::kStep, kq);
+            load(t[i], s + i + AHEAD);
+        }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (s + i < last)
+            t[i].add(acc, a, (s + i) * Tile::kStep, kq);
 #pragma unroll
     for (int r = 0; r < WR; ++r) {
         float unscale = kUnscale<BITS>;
