@@ -18,6 +18,12 @@ struct MatmulArgs {
     int64_t x_pitch, residual_pitch, y_pitch;
     int64_t w_row;               // bytes of a row of weights
 };
+// How the linear layer is cut: rows of x in tiles of 32 tf, rows of weights in
+// tiles of 128 wf, k in pieces of `columns`; tf = 0: the kernel for few rows.
+struct TilePlan {
+    int32_t tf, wf, splits, columns;
+};
+TilePlan plan_matmul(const MatmulArgs &a, int bits);
 hipError_t launch_matmul(const MatmulArgs &a, int type, int bits, void *ws, hipStream_t s);
 size_t matmul_workspace(const MatmulArgs &a, int type, int bits);
 

@@ -2,5 +2,8 @@
 #include "lm_matmul_impl.h"
 
 namespace qnn_lm {
-hipError_t launch_matmul_f16_w2(const MatmulArgs &a, hipStream_t s) { return launch_matmul_one<F16, 2>(a, s); }
+hipError_t launch_matmul_f16_w2(const MatmulArgs &a, void *ws, hipStream_t s)
+{
+    return launch_matmul_one<F16, 2>(a, ws, s);
+}
 }  // namespace qnn_lm

@@ -7,11 +7,10 @@
 namespace qnn_lm {
 
 template <class N, int BITS>
-hipError_t launch_matmul_one(const MatmulArgs &a, hipStream_t s)
+hipError_t launch_matmul_one(const MatmulArgs &a, void *ws, hipStream_t s)
 {
-    // the tile kernel's offsets within a tile are 32 bits
-    const bool near = a.x_pitch < 1 << 23 && a.w_row < 1 << 23;
-    return a.r > 64 && near ? launch_tile_bits<N, BITS>(a, s) : launch_rows_bits<N, BITS>(a, s);
+    const TilePlan p = plan_matmul(a, BITS);
+    return p.tf ? launch_tile_bits<N, BITS>(a, p, ws, s) : launch_rows_bits<N, BITS>(a, s);
 }
 
 }  // namespace qnn_lm

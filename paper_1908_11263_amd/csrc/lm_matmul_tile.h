@@ -76,7 +76,7 @@ struct TileShape {
     static constexpr int kXBytes = BM * kXRow, kWBytes = BN * kWRow;
     static constexpr int kStage = kXBytes + kWBytes + GPB * BN * 4;
     // two workgroups a compute unit
-    static constexpr int kStages = 3 * kStage <= 80 * 1024 ? 3 : 2;
+    static constexpr int kStages = 4 * kStage <= 64 * 1024 ? 4 : 3 * kStage <= 80 * 1024 ? 3 : 2;
     static constexpr int kOutPitch = BN + 4;                  // floats
     static constexpr int kOut = 32 * kOutPitch * 4;
     static constexpr int kLds = kStages * kStage > kOut ? kStages * kStage : kOut;
@@ -98,7 +98,9 @@ struct TileShape {
 };
 
 struct TileGrid {
-    int32_t tm, tn;  // tiles of rows of x, of rows of weights
+    int32_t tm, tn;         // tiles of rows of x, of rows of weights
+    int32_t splits, steps;  // pieces of k, of so many steps
+    float *part;            // [splits][r][rows of weights] sums, where there is more than one piece
 };
 
 // The products of eight F of a block.
@@ -133,7 +135,9 @@ template <class N, int BITS, int TF, int WF, int GPB, bool GATED>
 __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileGrid g)
 {
     using S = TileShape<BITS, TF, WF, GPB>;
-    static_assert(!GATED || WF == 2, "a wave holds a gate's rows and their partners");
+    // A gated layer's wave holds a gate's rows and their partners: two blocks of
+    // 32 (WF = 2), or the halves of one (WF = 1).
+    constexpr int GR = GATED ? 16 * WF : 0, HR = GATED ? GR : 1;  // rows of a wave's half
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -142,7 +146,8 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     // Tiles in an order that keeps an XCD (workgroups go round the eight of
     // them) on neighbouring tiles, eight tiles of x to a column of weights.
     const int32_t tiles = g.tm * g.tn;
-    int32_t t = blockIdx.x;
+    const int32_t split = blockIdx.x / tiles;
+    int32_t t = blockIdx.x - split * tiles;
     {
         const int32_t q = tiles >> 3, rem = tiles & 7, x = t & 7;
         t = x * q + min(x, rem) + (t >> 3);
@@ -168,25 +173,39 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     for (int i = 0; i < S::kWCopies; ++i) {
         const int e0 = (wave * S::kWCopies + i) * 64, e = e0 + lane, r = e / S::kWUnits;
         wc[i] = S::w_place(r, e % S::kWUnits);
+        wb[i] = (const uint8_t *)a.w + (int64_t)j0 * a.w_row;
         if constexpr (GATED) {
-            // staged row 64 w + 32 f + r is row 32 w + r of half f
-            const int j = j0 + (r >> 6) * 32 + (r & 31);
-            const int up = (e0 / S::kWUnits >> 5) & 1;
-            wb[i] = (const uint8_t *)a.w + (int64_t)up * a.m * a.w_row + (int64_t)j0 * a.w_row;
-            wo[i] = (uint32_t)(min(j, a.m - 1) - j0) * (uint32_t)a.w_row + wc[i] * S::kWUnit;
+            // staged row 2 GR w + GR f + r is row GR w + r of half f
+            const int j = min(j0 + r / (2 * HR) * HR + r % HR, a.m - 1) - j0;
+            if constexpr (WF == 2) {
+                const int up = (e0 / S::kWUnits >> 5) & 1;
+                wb[i] += (int64_t)up * a.m * a.w_row;
+                wo[i] = (uint32_t)j * (uint32_t)a.w_row + wc[i] * S::kWUnit;
+            } else {
+                // (a copy's rows lie in both halves: the launcher sees to 32 bits)
+                wo[i] = (uint32_t)((r / HR & 1) * a.m + j) * (uint32_t)a.w_row + wc[i] * S::kWUnit;
+            }
         } else {
-            wb[i] = (const uint8_t *)a.w + (int64_t)j0 * a.w_row;
             wo[i] = (uint32_t)(min(j0 + r, a.m - 1) - j0) * (uint32_t)a.w_row + wc[i] * S::kWUnit;
         }
     }
-    // scales: one a lane and group (of half wave / 2 where gated)
+    // scales: one a lane and group (gated: all of a half, then the other's)
     const float *sb = nullptr;
     uint32_t so = 0;
     if constexpr (GPB) {
         const int e = (WF == 2 ? wave : wave & 1) * 64 + lane;
-        const int up = GATED ? wave >> 1 : 0, j = GATED ? j0 + (e & 127) : j0 + e;
-        sb = a.scale + ((int64_t)up * a.m + j0) * a.groups;
-        so = (uint32_t)(min(j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
+        const int up = GATED ? e / (S::BN / 2) : 0, j = GATED ? e % (S::BN / 2) : e;
+        sb = a.scale + (int64_t)j0 * a.groups;
+        if constexpr (GATED) {
+            if constexpr (WF == 2) {
+                sb += (int64_t)(wave >> 1) * a.m * a.groups;
+                so = (uint32_t)(min(j0 + j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
+            } else {
+                so = (uint32_t)(up * a.m + min(j0 + j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
+            }
+        } else {
+            so = (uint32_t)(min(j0 + j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
+        }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
@@ -228,12 +247,12 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     for (int n = 0; n < WF; ++n)
         unit[n] = 1.f, clear[n] = 0;
 
-    const int32_t steps = (a.k + S::KS - 1) / S::KS;
+    const int32_t begin = split * g.steps, steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
 #pragma unroll
     for (int s = 0; s < S::kStages - 1; ++s)
-        issue(min(s, steps - 1), s);
+        issue(min(begin + s, steps - 1), s);
     int buf = 0;
-    for (int32_t s = 0; s < steps; ++s) {
+    for (int32_t s = begin; s < steps; ++s) {
         wait_copies<(S::kStages - 2) * S::kCopies>();
         __builtin_amdgcn_s_barrier();
         {
@@ -253,13 +272,15 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 if ((k & (a.group - 1)) == 0) {
 #pragma unroll
                     for (int n = 0; n < WF; ++n) {
-                        const float sc = ss[(GPB == 2 ? b * S::BN : 0) + (GATED ? n * 128 + wave * 32 : wave * 32 * WF + n * 32) + l32];
-                        const float ratio = k == 0 ? 0.f : unit[n] / sc;
+                        const int at = !GATED ? (wave * WF + n) * 32 + l32
+                                       : WF == 2 ? n * 128 + wave * 32 + l32 : (l32 >> 4) * 64 + wave * 16 + (l32 & 15);
+                        const float sc = ss[(GPB == 2 ? b * S::BN : 0) + at];
+                        const float ratio = k == begin * S::KS ? 0.f : unit[n] / sc;
                         const bool zero = sc == 0.f || __builtin_isinf(ratio);
                         clear[n] = zero ? 0xFFFFFFFFu : 0;
                         const float f = zero ? 1.f : ratio;
                         unit[n] = zero ? unit[n] : sc;
-                        if (k != 0)
+                        if (k != begin * S::KS)
 #pragma unroll
                             for (int m = 0; m < TF; ++m)
                                 acc[m][n] *= f;
@@ -304,16 +325,21 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     // memory, from where rows are written (and the residual read) 16 bytes a lane.
     float *out = (float *)lds;
     float bias[WF];
+    // (the largest tiles are taken where there are enough of them: never in pieces)
+    const bool pieces = TF < 4 && g.splits > 1;
+    const int64_t rows = GATED ? 2 * (int64_t)a.m : a.m;
 #pragma unroll
     for (int n = 0; n < WF; ++n) {
-        const int32_t j = min(j0 + (GATED ? wave * 32 : (wave * WF + n) * 32) + l32, a.m - 1);
-        const int64_t row = GATED && n ? (int64_t)a.m + j : j;
+        const int q = n * 32 + l32;  // row of this wave
+        const int32_t j = min(j0 + (GATED ? wave * GR + q % HR : wave * WF * 32 + q), a.m - 1);
+        const int64_t row = GATED && q >= GR ? (int64_t)a.m + j : j;
         unit[n] *= kUnscale<BITS>;
         if (BITS != 16 && !GPB)
             unit[n] *= a.scale[row];
-        bias[n] = a.bias ? a.bias[row] : 0.f;
+        bias[n] = a.bias && !pieces ? a.bias[row] : 0.f;
     }
-    const bool wide = ((a.m | (int32_t)a.y_pitch | (a.residual ? (int32_t)a.residual_pitch : 0)) & 7) == 0;
+    const bool wide = pieces ? (a.m & 7) == 0
+                             : ((a.m | (int32_t)a.y_pitch | (a.residual ? (int32_t)a.residual_pitch : 0)) & 7) == 0;
 #pragma unroll
     for (int m = 0; m < TF; ++m) {
         if (r0 + m * 32 >= a.r)
@@ -322,78 +348,154 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
             __syncthreads();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float *p = out + (8 * (i / 4) + 4 * half + i % 4) * S::kOutPitch + l32;
-            if constexpr (GATED) {
-                p[wave * 32] = activate(acc[m][0][i] * unit[0] + bias[0], a.act) * (acc[m][1][i] * unit[1] + bias[1]);
+            float *p = out + (8 * (i / 4) + 4 * half + i % 4) * S::kOutPitch;
+            if (GATED && WF == 2 && !pieces) {
+                p[wave * 32 + l32] =
+                    activate(acc[m][0][i] * unit[0] + bias[0], a.act) * (acc[m][WF - 1][i] * unit[WF - 1] + bias[WF - 1]);
+            } else if (GATED && !pieces) {
+                // the partner's sum is 16 lanes on
+                const float v = acc[m][0][i] * unit[0] + bias[0], up = __shfl_down(v, 16, 32);
+                if (l32 < 16)
+                    p[wave * 16 + l32] = activate(v, a.act) * up;
             } else {
 #pragma unroll
-                for (int n = 0; n < WF; ++n)
-                    p[(wave * WF + n) * 32] = activate(acc[m][n][i] * unit[n] + bias[n], a.act);
+                for (int n = 0; n < WF; ++n) {
+                    const float v = acc[m][n][i] * unit[n] + bias[n];
+                    p[(wave * WF + n) * 32 + l32] = pieces ? v : activate(v, a.act);
+                }
             }
         }
         __syncthreads();
-        constexpr int LANES = OUT / 8;  // of a row
+        if (wide) {
+            const int lanes = (pieces ? S::BN : OUT) / 8;  // of a row
 #pragma unroll 1
-        for (int r = threadIdx.x / LANES; r < 32; r += 256 / LANES) {
-            const int64_t row = r0 + m * 32 + r;
-            const int32_t col = j0 + threadIdx.x % LANES * 8;
-            if (row >= a.r || col >= a.m)
-                continue;
-            float v[8], res[8];
-            load8<F32>(out, r * S::kOutPitch + threadIdx.x % LANES * 8, v);
-            if (wide) {
+            for (int r = threadIdx.x / lanes; r < 32; r += 256 / lanes) {
+                const int64_t row = r0 + m * 32 + r;
+                const int c = threadIdx.x % lanes * 8;
+                // (pieces: staged rows 2 GR w + GR f + r of a gated layer)
+                const int32_t col = j0 + (GATED && pieces ? c / (2 * HR) * HR + c % HR : c);
+                if (row >= a.r || col >= a.m)
+                    continue;
+                float v[8];
+                load8<F32>(out, r * S::kOutPitch + c, v);
+                if (pieces) {
+                    store8<F32>(g.part, (split * a.r + row) * rows + (GATED && (c / HR & 1) ? a.m : 0) + col, v);
+                    continue;
+                }
                 if (a.residual) {
+                    float res[8];
                     load8<N>(a.residual, row * a.residual_pitch + col, res);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         v[e] += res[e];
                 }
                 store8<N>(a.y, row * a.y_pitch + col, v);
-            } else {
-                for (int e = 0; e < 8 && col + e < a.m; ++e) {
-                    if (a.residual)
-                        v[e] += load1<N>(a.residual, row * a.residual_pitch + col + e);
-                    store1<N>(a.y, row * a.y_pitch + col + e, v[e]);
+            }
+        } else {
+            // rows that start anywhere: a lane a column
+            const int lanes = pieces ? S::BN : OUT;
+#pragma unroll 1
+            for (int e = threadIdx.x; e < 32 * lanes; e += 256) {
+                const int c = e % lanes, r = e / lanes;
+                const int64_t row = r0 + m * 32 + r;
+                const int32_t col = j0 + (GATED && pieces ? c / (2 * HR) * HR + c % HR : c);
+                if (row >= a.r || col >= a.m)
+                    continue;
+                float v = out[r * S::kOutPitch + c];
+                if (pieces) {
+                    g.part[(split * a.r + row) * rows + (GATED && (c / HR & 1) ? a.m : 0) + col] = v;
+                    continue;
                 }
+                if (a.residual)
+                    v += load1<N>(a.residual, row * a.residual_pitch + col);
+                store1<N>(a.y, row * a.y_pitch + col, v);
             }
         }
     }
 }
 
+// Sums the pieces of k in their order and finishes; a thread four outputs.
+template <class N>
+__global__ void __launch_bounds__(256) matmul_join_kernel(MatmulArgs a, int32_t splits, const float *part)
+{
+    const int32_t quads = (a.m + 3) >> 2;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = i / quads;
+    const int32_t col = (int32_t)(i - row * quads) * 4;
+    if (row >= a.r)
+        return;
+    const int64_t rows = a.gated ? 2 * (int64_t)a.m : a.m, all = a.r * rows;
+    const float *p = part + row * rows + col;
+    f4 t = {0, 0, 0, 0}, up = {0, 0, 0, 0};
+    if (a.m % 4 == 0) {
+        for (int s = 0; s < splits; ++s) {
+            t += *(const f4 *)(p + s * all);
+            if (a.gated)
+                up += *(const f4 *)(p + s * all + a.m);
+        }
+    } else {
+        for (int s = 0; s < splits; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < a.m) {
+                    t[e] += p[s * all + e];
+                    if (a.gated)
+                        up[e] += p[s * all + a.m + e];
+                }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (col + e < a.m)
+            finish<N>(a, row, col + e, t[e], up[e]);
+}
+
 template <class N, int BITS, int TF, int WF, int GPB, bool GATED>
-hipError_t launch_tile(const MatmulArgs &a, hipStream_t s)
+hipError_t launch_tile(const MatmulArgs &a, const TilePlan &p, void *ws, hipStream_t s)
 {
     using S = TileShape<BITS, TF, WF, GPB>;
     constexpr int OUT = GATED ? S::BN / 2 : S::BN;
     TileGrid g;
     g.tm = (a.r + S::BM - 1) / S::BM;
     g.tn = (a.m + OUT - 1) / OUT;
+    g.splits = p.splits;
+    g.steps = p.columns / S::KS;
+    g.part = (float *)ws;
     const void *kernel = (const void *)matmul_tile_kernel<N, BITS, TF, WF, GPB, GATED>;
     if constexpr (S::kLds > 64 * 1024) {
         static std::atomic<uint64_t> devices{0};
         qnn::allow_large_lds(kernel, devices);
     }
-    hipLaunchKernelGGL((matmul_tile_kernel<N, BITS, TF, WF, GPB, GATED>), dim3((unsigned)g.tm * g.tn), dim3(256), S::kLds,
-                       s, a, g);
+    hipLaunchKernelGGL((matmul_tile_kernel<N, BITS, TF, WF, GPB, GATED>), dim3((unsigned)(g.tm * g.tn * g.splits)), dim3(256),
+                       S::kLds, s, a, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.splits == 1)
+        return e;
+    const int64_t threads = (int64_t)a.r * ((a.m + 3) / 4);
+    hipLaunchKernelGGL(matmul_join_kernel<N>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, g.splits, g.part);
     return hipGetLastError();
 }
 
-template <class N, int BITS, int GPB>
-hipError_t launch_tile_groups(const MatmulArgs &a, hipStream_t s)
+template <class N, int BITS, int TF, int WF>
+hipError_t launch_tile_sized(const MatmulArgs &a, const TilePlan &p, void *ws, hipStream_t s)
 {
-    if (a.gated)
-        return launch_tile<N, BITS, 4, 2, GPB, true>(a, s);
-    return launch_tile<N, BITS, 4, 2, GPB, false>(a, s);
+    if constexpr (BITS != 16) {
+        if (a.groups > 1 && a.group == 32)
+            return a.gated ? launch_tile<N, BITS, TF, WF, 2, true>(a, p, ws, s) : launch_tile<N, BITS, TF, WF, 2, false>(a, p, ws, s);
+        if (a.groups > 1)
+            return a.gated ? launch_tile<N, BITS, TF, WF, 1, true>(a, p, ws, s) : launch_tile<N, BITS, TF, WF, 1, false>(a, p, ws, s);
+    }
+    return a.gated ? launch_tile<N, BITS, TF, WF, 0, true>(a, p, ws, s) : launch_tile<N, BITS, TF, WF, 0, false>(a, p, ws, s);
 }
 
 template <class N, int BITS>
-hipError_t launch_tile_bits(const MatmulArgs &a, hipStream_t s)
+hipError_t launch_tile_bits(const MatmulArgs &a, const TilePlan &p, void *ws, hipStream_t s)
 {
-    if constexpr (BITS != 16) {
-        if (a.groups > 1)
-            return a.group == 32 ? launch_tile_groups<N, BITS, 2>(a, s) : launch_tile_groups<N, BITS, 1>(a, s);
-    }
-    return launch_tile_groups<N, BITS, 0>(a, s);
+    if constexpr (BITS != 16)
+        if (p.tf == 1)
+            return launch_tile_sized<N, BITS, 1, 1>(a, p, ws, s);
+    if (p.tf == 2)
+        return p.wf == 1 ? launch_tile_sized<N, BITS, 2, 1>(a, p, ws, s) : launch_tile_sized<N, BITS, 2, 2>(a, p, ws, s);
+    return launch_tile_sized<N, BITS, 4, 2>(a, p, ws, s);
 }
 
 }  // namespace qnn_lm
