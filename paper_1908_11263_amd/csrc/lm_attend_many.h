@@ -31,12 +31,12 @@ struct ManyShape {
     static constexpr int groups(int nr) { return BITS == 16 && (nr == 2 || DIM == 256) ? 1 : 2; }
     // Tiles that are loaded ahead, one set of registers each.
     static constexpr int kAhead = BITS == 16 ? 1 : 2;
-    // place of piece c of row r: eight rows that read one piece, four that read
-    // two neighbouring ones, and eight lanes that write one or two rows' every
-    // second or fourth piece find different banks
+    // Place of piece c of row r.  256 bytes of local memory answer at once: the
+    // sixteen rows of which one piece is read (K), and the eight of which two
+    // neighbouring ones are (V), have them at different places of 256 bytes.
     static __device__ __forceinline__ int place(int r, int c)
     {
-        return c ^ (((r & 3) << 1) | ((r >> 2) & 1)) ^ ((c >> 3) & 1);
+        return c ^ (DIM == 64 ? ((r >> 1) & 3) << 1 | ((r >> 3) & 1) : (r & 7) << 1 | ((r >> 3) & 1));
     }
 };
 

@@ -81,17 +81,19 @@ struct TileShape {
     static constexpr int kOut = 32 * kOutPitch * 4;
     static constexpr int kLds = kStages * kStage > kOut ? kStages * kStage : kOut;
 
-    // place of piece c of row r among the row's pieces
+    // Place of piece c of row r among the row's pieces: 256 bytes of local memory
+    // answer at once, so the pieces that sixteen neighbouring lanes read, one a
+    // row, have to lie at sixteen different places of 256 bytes.
     static __device__ __forceinline__ int x_place(int r, int c)
     {
-        return c ^ (kXChunks == 8 ? r & 7 : (r >> 1) & 3);
+        return c ^ (kXChunks == 8 ? (r >> 1) & 7 : (r >> 2) & 3);
     }
     static __device__ __forceinline__ int w_place(int r, int c)
     {
         if constexpr (BITS == 8 || BITS == 16)  // four pieces
-            return c ^ ((r >> 1) & 3);
+            return c ^ ((r >> 2) & 3);
         else if constexpr (BITS == 4)
-            return c ^ ((r >> 2) & 1);
+            return c ^ ((r >> 3) & 1);
         else
             return c;
     }
@@ -103,32 +105,66 @@ struct TileGrid {
     float *part;            // [splits][r][rows of weights] sums, where there is more than one piece
 };
 
-// The products of eight F of a block.
+// Operands of one eight: every second one of a wave's is in flight while the
+// other is multiplied.
+template <class N, int TF, int WF>
+struct Eight {
+    typename N::V8 x[TF], w[WF];
+};
+
+// Codes of one block, as they lie in local memory.
+template <int BITS, int WF>
+struct Raw {
+    uint32_t w[WF][BITS >= 2 ? BITS / 2 : 1];
+};
+
+// Reads x and expands the codes of eight F of block b.
 template <class N, int BITS, int TF, int WF, int GPB, int F>
-__device__ __forceinline__ void eights(const uint8_t *xs, const uint32_t (&raw)[WF][BITS >= 2 ? BITS / 2 : 1],
-                                       const uint32_t (&clear)[WF], f16v (&acc)[TF][WF], int b, int l32, int half)
+__device__ __forceinline__ void fetch(const uint8_t *xs, const Raw<BITS, WF> &raw, const uint32_t (&clear)[WF], int b,
+                                      int l32, int half, Eight<N, TF, WF> &e)
 {
     using S = TileShape<BITS, TF, WF, GPB>;
-    typename N::V8 x[TF], w[WF];
 #pragma unroll
     for (int m = 0; m < TF; ++m) {
         const int r = m * 32 + l32;
-        x[m] = *(const typename N::V8 *)(xs + r * S::kXRow + S::x_place(r, 4 * b + 2 * half + F) * 16);
+        e.x[m] = *(const typename N::V8 *)(xs + r * S::kXRow + S::x_place(r, 4 * b + 2 * half + F) * 16);
     }
 #pragma unroll
     for (int n = 0; n < WF; ++n) {
-        w[n] = expand<N, BITS, F>(raw[n]);
+        uint32_t w[BITS >= 2 ? BITS / 2 : 1];
+#pragma unroll
+        for (int i = 0; i < (BITS >= 2 ? BITS / 2 : 1); ++i)
+            // (a 1-bit code has no zero: its numbers are cleared instead)
+            w[i] = GPB && BITS != 1 ? raw.w[n][i] & ~clear[n] : raw.w[n][i];
+        e.w[n] = expand<N, BITS, F>(w);
         if constexpr (GPB && BITS == 1) {
-            u4 v = __builtin_bit_cast(u4, w[n]);
+            u4 v = __builtin_bit_cast(u4, e.w[n]);
             v &= ~clear[n];
-            w[n] = __builtin_bit_cast(typename N::V8, v);
+            e.w[n] = __builtin_bit_cast(typename N::V8, v);
         }
     }
+}
+
+template <class N, int TF, int WF>
+__device__ __forceinline__ void products(const Eight<N, TF, WF> &e, f16v (&acc)[TF][WF])
+{
 #pragma unroll
     for (int n = 0; n < WF; ++n)
 #pragma unroll
         for (int m = 0; m < TF; ++m)
-            acc[m][n] = mfma32(x[m], w[n], acc[m][n]);
+            acc[m][n] = mfma32(e.x[m], e.w[n], acc[m][n]);
+}
+
+// Asks for what multiplies and what prepares the next eight to alternate.
+template <int PRODUCTS>
+__device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // reads of local memory
+        __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);  // vector instructions
+    }
 }
 
 template <class N, int BITS, int TF, int WF, int GPB, bool GATED>
@@ -213,17 +249,26 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         const int32_t k0 = step * S::KS, left = a.k - k0;  // a multiple of 32
         const uint32_t at = lds0 + buf * S::kStage;
         const uint8_t *x = xb + (int64_t)k0 * 2;
-        const bool whole = left >= S::KS;
+        const int64_t w = (int64_t)k0 * BITS / 8;
+        const uint32_t xat = at + wave * S::kXCopies * 1024,
+                       wat = at + S::kXBytes + wave * S::kWCopies * 64 * S::kWUnit;
+        if (left >= S::KS) {
 #pragma unroll
-        for (int i = 0; i < S::kXCopies; ++i)
-            // (pieces past the row's end, never read, copy its first again)
-            copy_to_lds<16>(x, whole || xc[i] * 8 < left ? xo[i] : xo[i] - xc[i] * 16,
-                            at + (wave * S::kXCopies + i) * 1024);
+            for (int i = 0; i < S::kXCopies; ++i)
+                copy_to_lds<16>(x, xo[i], xat + i * 1024);
 #pragma unroll
-        for (int i = 0; i < S::kWCopies; ++i)
-            copy_to_lds<S::kWUnit>(wb[i] + (int64_t)k0 * BITS / 8,
-                                   whole || wc[i] * (S::kWUnit * 8 / BITS) < left ? wo[i] : wo[i] - wc[i] * S::kWUnit,
-                                   at + S::kXBytes + (wave * S::kWCopies + i) * 64 * S::kWUnit);
+            for (int i = 0; i < S::kWCopies; ++i)
+                copy_to_lds<S::kWUnit>(wb[i] + w, wo[i], wat + i * 64 * S::kWUnit);
+        } else {
+            // pieces past the row's end, never read, copy its first again
+#pragma unroll
+            for (int i = 0; i < S::kXCopies; ++i)
+                copy_to_lds<16>(x, xc[i] * 8 < left ? xo[i] : xo[i] - xc[i] * 16, xat + i * 1024);
+#pragma unroll
+            for (int i = 0; i < S::kWCopies; ++i)
+                copy_to_lds<S::kWUnit>(wb[i] + w, wc[i] * (S::kWUnit * 8 / BITS) < left ? wo[i] : wo[i] - wc[i] * S::kWUnit,
+                                       wat + i * 64 * S::kWUnit);
+        }
         if constexpr (GPB) {
             const int32_t grp = k0 >> __builtin_ctz(a.group);
 #pragma unroll
@@ -248,73 +293,120 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         unit[n] = 1.f, clear[n] = 0;
 
     const int32_t begin = split * g.steps, steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
+    float f[WF];  // old unit over new, of the group that begins
 #pragma unroll
-    for (int s = 0; s < S::kStages - 1; ++s)
-        issue(min(begin + s, steps - 1), s);
-    int buf = 0;
-    for (int32_t s = begin; s < steps; ++s) {
-        wait_copies<(S::kStages - 2) * S::kCopies>();
-        __builtin_amdgcn_s_barrier();
-        {
-            // (past the last step it is copied again, so that the counts stay)
-            const int to = buf == 0 ? S::kStages - 1 : buf - 1;
-            issue(min(s + S::kStages - 1, steps - 1), to);
-        }
-        const uint8_t *xs = lds + buf * S::kStage, *ws = xs + S::kXBytes;
-        const float *ss = (const float *)(ws + S::kWBytes);
-        const int blocks = min(a.k - s * S::KS, S::KS) >> 5;
+    for (int n = 0; n < WF; ++n)
+        f[n] = 1.f;
+    constexpr int BLOCKS = S::KS / 32;
+    Raw<BITS, WF> raw[BLOCKS];
+    Eight<N, TF, WF> pair[2];
+    auto read_raw = [&](const uint8_t *ws) {
 #pragma unroll
-        for (int b = 0; b < S::KS / 32; ++b) {
-            if (b >= blocks)
-                break;
-            if constexpr (GPB) {
-                const int32_t k = s * S::KS + b * 32;
-                if ((k & (a.group - 1)) == 0) {
-#pragma unroll
-                    for (int n = 0; n < WF; ++n) {
-                        const int at = !GATED ? (wave * WF + n) * 32 + l32
-                                       : WF == 2 ? n * 128 + wave * 32 + l32 : (l32 >> 4) * 64 + wave * 16 + (l32 & 15);
-                        const float sc = ss[(GPB == 2 ? b * S::BN : 0) + at];
-                        const float ratio = k == begin * S::KS ? 0.f : unit[n] / sc;
-                        const bool zero = sc == 0.f || __builtin_isinf(ratio);
-                        clear[n] = zero ? 0xFFFFFFFFu : 0;
-                        const float f = zero ? 1.f : ratio;
-                        unit[n] = zero ? unit[n] : sc;
-                        if (k != begin * S::KS)
-#pragma unroll
-                            for (int m = 0; m < TF; ++m)
-                                acc[m][n] *= f;
-                    }
-                }
-            }
-            uint32_t raw[WF][BITS >= 2 ? BITS / 2 : 1];
+        for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int n = 0; n < WF; ++n) {
                 const int r = (wave * WF + n) * 32 + l32;
                 const uint8_t *p = ws + r * S::kWRow;
+                uint32_t *to = raw[b].w[n];
                 if constexpr (BITS == 16) {
 #pragma unroll
-                    for (int f = 0; f < 2; ++f)
-                        load_words<4>(p + S::w_place(r, 2 * half + f) * 16, raw[n] + 4 * f);
+                    for (int h = 0; h < 2; ++h)
+                        load_words<4>(p + S::w_place(r, 2 * half + h) * 16, to + 4 * h);
                 } else if constexpr (BITS == 8) {
-                    load_words<4>(p + S::w_place(r, 2 * b + half) * 16, raw[n]);
+                    load_words<4>(p + S::w_place(r, 2 * b + half) * 16, to);
                 } else if constexpr (BITS == 4) {
-                    load_words<2>(p + S::w_place(r, b) * 16 + half * 8, raw[n]);
+                    load_words<2>(p + S::w_place(r, b) * 16 + half * 8, to);
                 } else {
-                    load_raw<2 * BITS>(p + b * 4 * BITS + half * 2 * BITS, raw[n]);
+                    load_raw<2 * BITS>(p + b * 4 * BITS + half * 2 * BITS, to);
                 }
             }
-            // (a 1-bit code has no zero: its numbers are cleared instead)
-            if constexpr (GPB && BITS != 1)
+    };
+    // Whether block b of step s begins a group; if so its scale is the new unit.
+    auto begins = [&](int32_t s, int b, const uint8_t *ws) {
+        if constexpr (!GPB) {
+            return false;
+        } else {
+            const int32_t k = s * S::KS + b * 32;
+            if (k & (a.group - 1))
+                return false;
+            const float *ss = (const float *)(ws + S::kWBytes);
 #pragma unroll
-                for (int n = 0; n < WF; ++n)
-#pragma unroll
-                    for (uint32_t &w : raw[n])
-                        w &= ~clear[n];
-            eights<N, BITS, TF, WF, GPB, 0>(xs, raw, clear, acc, b, l32, half);
-            eights<N, BITS, TF, WF, GPB, 1>(xs, raw, clear, acc, b, l32, half);
+            for (int n = 0; n < WF; ++n) {
+                const int at = !GATED ? (wave * WF + n) * 32 + l32
+                               : WF == 2 ? n * 128 + wave * 32 + l32 : (l32 >> 4) * 64 + wave * 16 + (l32 & 15);
+                const float sc = ss[(GPB == 2 ? b * S::BN : 0) + at];
+                const float ratio = k == begin * S::KS ? 0.f : unit[n] / sc;
+                const bool zero = sc == 0.f || __builtin_isinf(ratio);
+                clear[n] = zero ? 0xFFFFFFFFu : 0;
+                f[n] = zero || k == begin * S::KS ? 1.f : ratio;
+                unit[n] = zero ? unit[n] : sc;
+            }
+            return true;
         }
+    };
+    auto rescale = [&] {
+#pragma unroll
+        for (int m = 0; m < TF; ++m)
+#pragma unroll
+            for (int n = 0; n < WF; ++n)
+                acc[m][n] *= f[n];
+    };
+    // (no branch between an eight's products and the next one's preparation:
+    // they are to alternate)
+    auto multiply = [&](const Eight<N, TF, WF> &e) {
+        products<N, TF, WF>(e, acc);
+        interleave<TF * WF>();
+    };
+
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s)
+        issue(min(begin + s, steps - 1), s);
+    wait_copies<(S::kStages - 2) * S::kCopies>();
+    __builtin_amdgcn_s_barrier();
+    issue(min(begin + S::kStages - 1, steps - 1), S::kStages - 1);
+    int buf = 0;
+    read_raw(lds + S::kXBytes);
+    bool scale = begins(begin, 0, lds + S::kXBytes);
+    fetch<N, BITS, TF, WF, GPB, 0>(lds, raw[0], clear, 0, l32, half, pair[0]);
+    // (k is a multiple of 32: the last step of all may be one block)
+    const bool half_step = BLOCKS == 2 && steps * S::KS > a.k;
+    const int32_t whole = half_step ? steps - 1 : steps;
+    for (int32_t s = begin; s < whole; ++s) {
+        const uint8_t *xs = lds + buf * S::kStage;
+        if (GPB && scale)
+            rescale();
+        fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
+        multiply(pair[0]);
+        if constexpr (BLOCKS == 2) {
+            if constexpr (GPB == 2)
+                begins(s, 1, xs + S::kXBytes);
+            fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, pair[0]);
+            multiply(pair[1]);
+            if constexpr (GPB == 2)
+                rescale();
+            fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[1], clear, 1, l32, half, pair[1]);
+            multiply(pair[0]);
+        }
+        // Everything of this step has been read: the next one's copies are
+        // waited for, and this one's place is filled again (past the last step
+        // with the last one, so that the counts stay).
+        wait_copies<(S::kStages - 2) * S::kCopies>();
+        __builtin_amdgcn_s_barrier();
+        issue(min(s + S::kStages, steps - 1), buf);
         buf = buf == S::kStages - 1 ? 0 : buf + 1;
+        const uint8_t *xn = lds + buf * S::kStage;
+        read_raw(xn + S::kXBytes);
+        scale = s + 1 < steps && begins(s + 1, 0, xn + S::kXBytes);
+        fetch<N, BITS, TF, WF, GPB, 0>(xn, raw[0], clear, 0, l32, half, pair[0]);
+        multiply(pair[1]);
+    }
+    if (half_step) {
+        const uint8_t *xs = lds + buf * S::kStage;
+        if (GPB && scale)
+            rescale();
+        fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
+        multiply(pair[0]);
+        multiply(pair[1]);
     }
     // the copies of the last steps, made again, are there before local memory
     // is used anew
