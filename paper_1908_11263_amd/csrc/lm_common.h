@@ -231,6 +231,27 @@ __device__ __forceinline__ void load8(const void *p, int64_t i, float (&v)[8])
     }
 }
 
+// ... from and to any place of 16-bit numbers (the memory unit takes 16 bytes
+// at any address).
+typedef u4 u4_any __attribute__((aligned(2)));
+
+template <class N>
+__device__ __forceinline__ void load8_any(const void *p, int64_t i, float (&v)[8])
+{
+    const u4 r = *(const u4_any *)((const typename N::T *)p + i);
+    const typename N::V8 a = __builtin_bit_cast(typename N::V8, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = (float)a[e];
+}
+
+template <class N>
+__device__ __forceinline__ void store8_any(void *p, int64_t i, const float (&v)[8])
+{
+    const u4 r = {pack2<N>(v[0], v[1]), pack2<N>(v[2], v[3]), pack2<N>(v[4], v[5]), pack2<N>(v[6], v[7])};
+    *(u4_any *)((typename N::T *)p + i) = r;
+}
+
 template <class N>
 __device__ __forceinline__ void store8(void *p, int64_t i, const float (&v)[8])
 {

@@ -430,8 +430,7 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
             unit[n] *= a.scale[row];
         bias[n] = a.bias && !pieces ? a.bias[row] : 0.f;
     }
-    const bool wide = pieces ? (a.m & 7) == 0
-                             : ((a.m | (int32_t)a.y_pitch | (a.residual ? (int32_t)a.residual_pitch : 0)) & 7) == 0;
+    const bool wide = !pieces || (a.m & 7) == 0;  // (sums of pieces are written whole quads or one by one)
 #pragma unroll
     for (int m = 0; m < TF; ++m) {
         if (r0 + m * 32 >= a.r)
@@ -474,33 +473,33 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                     store8<F32>(g.part, (split * a.r + row) * rows + (GATED && (c / HR & 1) ? a.m : 0) + col, v);
                     continue;
                 }
+                if (col + 8 > a.m) {
+                    for (int e = 0; col + e < a.m; ++e) {
+                        if (a.residual)
+                            v[e] += load1<N>(a.residual, row * a.residual_pitch + col + e);
+                        store1<N>(a.y, row * a.y_pitch + col + e, v[e]);
+                    }
+                    continue;
+                }
                 if (a.residual) {
                     float res[8];
-                    load8<N>(a.residual, row * a.residual_pitch + col, res);
+                    load8_any<N>(a.residual, row * a.residual_pitch + col, res);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         v[e] += res[e];
                 }
-                store8<N>(a.y, row * a.y_pitch + col, v);
+                store8_any<N>(a.y, row * a.y_pitch + col, v);
             }
         } else {
-            // rows that start anywhere: a lane a column
-            const int lanes = pieces ? S::BN : OUT;
+            // sums of rows of any length: a lane a column
 #pragma unroll 1
-            for (int e = threadIdx.x; e < 32 * lanes; e += 256) {
-                const int c = e % lanes, r = e / lanes;
+            for (int e = threadIdx.x; e < 32 * S::BN; e += 256) {
+                const int c = e % S::BN, r = e / S::BN;
                 const int64_t row = r0 + m * 32 + r;
-                const int32_t col = j0 + (GATED && pieces ? c / (2 * HR) * HR + c % HR : c);
-                if (row >= a.r || col >= a.m)
-                    continue;
-                float v = out[r * S::kOutPitch + c];
-                if (pieces) {
-                    g.part[(split * a.r + row) * rows + (GATED && (c / HR & 1) ? a.m : 0) + col] = v;
-                    continue;
-                }
-                if (a.residual)
-                    v += load1<N>(a.residual, row * a.residual_pitch + col);
-                store1<N>(a.y, row * a.y_pitch + col, v);
+                const int32_t col = j0 + (GATED ? c / (2 * HR) * HR + c % HR : c);
+                if (row < a.r && col < a.m)
+                    g.part[(split * a.r + row) * rows + (GATED && (c / HR & 1) ? a.m : 0) + col] =
+                        out[r * S::kOutPitch + c];
             }
         }
     }
