@@ -2,7 +2,9 @@
 
 Every HIP source under csrc/ is compiled for gfx950 only and linked into one
 shared library next to this file.  Packed-FP32 instruction generation is
-switched off for all device code.
+switched off for all device code.  The compiled part of the binding
+(csrc/lm_bind.cpp) is host code for torch's C++ headers: a module of its own,
+``_lm_bind.so``.
 """
 import concurrent.futures
 import os
@@ -15,6 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libqnn.so")
+BINDING = os.path.join(HERE, "_lm_bind.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -47,13 +50,40 @@ def _compile(src):
     return obj
 
 
+def build_binding():
+    """Compile the host's path of lm.py's calls (csrc/lm_bind.cpp) against torch's headers."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    rocm = os.path.dirname(os.path.dirname(HIPCC))
+    tmp = BINDING + ".tmp%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-sign-compare",
+           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-I" + INCLUDE,
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(rocm, "include")]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    cmd += [os.path.join(CSRC, "lm_bind.cpp"), "-o", tmp]
+    for path in cpp_extension.library_paths():
+        cmd += ["-L" + path, "-Wl,-rpath," + path]
+    cmd += ["-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for lm_bind.cpp:\n%s%s" % (r.stdout, r.stderr))
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(jobs=None, verbose=True):
-    """Compile every HIP source and link libqnn.so (always recompiles)."""
+    """Compile every HIP source, link libqnn.so and build the binding (always recompiles)."""
     os.makedirs(BUILD, exist_ok=True)
     srcs = sources()
     jobs = jobs or min(len(srcs), max(1, (os.cpu_count() or 2) // 2))
     with concurrent.futures.ThreadPoolExecutor(jobs) as ex:
+        binding = ex.submit(build_binding)
         objs = list(ex.map(_compile, srcs))
+        binding.result()
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -1,7 +1,9 @@
 """include/qnn_lm.h without a GPU: the library exports what the header
 declares, its arguments are checked on the host before any device call, and
 the binding refuses tensors that are not what a call takes."""
+import ctypes
 import re
+import struct
 
 import pytest
 import torch
@@ -11,8 +13,40 @@ P = 1 << 20  # a 16-byte aligned address that is never read
 BF, HF, F, I = torch.bfloat16, torch.float16, torch.float32, torch.int32
 
 
+class Raw:
+    """The library's entry points with plain arguments, and the C structures as packed bytes."""
+    _pack_linear = staticmethod(struct.Struct("@8i3q").pack)
+    _pack_norms = staticmethod(struct.Struct("@7i3f2q").pack)
+    _pack_cache = staticmethod(struct.Struct("@6i6q5P2i").pack)
+    _pack_queries = staticmethod(struct.Struct("@3if3q").pack)
+    _pack_tokens = staticmethod(struct.Struct("@2i6q").pack)
+
+    def __init__(self):
+        from paper_1908_11263_amd import lm, qnn
+        self.HEADER = lm.HEADER
+        P, I, S, Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_char_p, ctypes.c_size_t
+        arguments = {"qnn_lm_matmul": [S, P, P, P, P, P, P, P, Z, P], "qnn_lm_matmul_workspace": [S],
+                     "qnn_lm_norm_residual": [S] + 10 * [P], "qnn_lm_tree_attention": [S, P, S, P, P, P, P, P, P, Z, P],
+                     "qnn_lm_tree_attention_workspace": [S, S], "qnn_lm_cache_append": [S, P, P, S, P, P, P],
+                     "qnn_lm_cache_keep": [S, I, P, P, P, P], "qnn_lm_cache_read": [S, I, I, P, P, P, P]}
+        assert sorted(arguments) == sorted(lm.ENTRIES)
+        self.f = {}
+        for name, types in arguments.items():
+            f = qnn.lib()[name]
+            f.restype, f.argtypes = Z if name.endswith("workspace") else ctypes.c_int, types
+            self.f[name] = f
+
+    def _fn(self, name):
+        return self.f[name]
+
+
 @pytest.fixture(scope="module")
 def lm():
+    return Raw()
+
+
+@pytest.fixture(scope="module")
+def binding():
     from paper_1908_11263_amd import lm
     return lm
 
@@ -184,7 +218,8 @@ def refused(f, *args, **kw):
         f(*args, **kw)
 
 
-def test_binding_refuses(lm):
+def test_binding_refuses(binding):
+    lm = binding
     z = torch.zeros
     x, w, s = z(3, 64, dtype=BF), z(8, 32, dtype=torch.uint8), z(8)
     for bad in (dict(x=z(3, 64)), dict(x=z(64, 3, dtype=BF).t()), dict(w=z(8, 31, dtype=torch.uint8)), dict(w=z(8, 32)),
