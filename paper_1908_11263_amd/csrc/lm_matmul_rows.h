@@ -18,11 +18,11 @@
 
 namespace qnn_lm {
 
-template <class N, int BITS, int NF, int WR, int NC, bool GATED>
+template <class N, int BITS, int NF, int WR, int NC, bool GATED, bool XL>
 struct RowsTile {
     static constexpr int kStep = 32 * NF;
     uint32_t w[WR][kRaw<BITS, NF> < 4 ? 1 : kRaw<BITS, NF> / 4];
-    typename N::V8 x[NC][NF];
+    typename N::V8 x[XL ? 1 : NC][XL ? 1 : NF];  // XL: x lies in local memory
     float scale[WR];
 
     // (Never skipped: behind a branch that may skip a load, a wait for an older
@@ -40,24 +40,29 @@ struct RowsTile {
             if constexpr (BITS != 16)
                 scale[r] = sp[r][a.groups > 1 ? k0 >> __builtin_ctz(a.group) : 0];
         }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-                x[c][f] = *(const typename N::V8 *)(xp[c] + k + 8 * f);
-    }
-
-    __device__ __forceinline__ void add(f4 (&acc)[WR][NC], const MatmulArgs &a, int32_t k0, int kq)
-    {
-        const bool grouped = BITS != 16 && a.groups > 1;
-        if (k0 + kStep > a.k && k0 + kq * 8 * NF >= a.k) {
-            // (a code is finite whatever its bits, a 16-bit weight need not be)
-            const u4 zero = {0, 0, 0, 0};
+        if constexpr (!XL)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
-                    x[c][f] = __builtin_bit_cast(typename N::V8, zero);
+                    x[c][f] = *(const typename N::V8 *)(xp[c] + k + 8 * f);
+    }
+
+    // xl: this lane's row of x in local memory (XL), zero past k.
+    __device__ __forceinline__ void add(f4 (&acc)[WR][NC], const MatmulArgs &a, int32_t k0, int kq,
+                                        const typename N::T *xl)
+    {
+        const bool grouped = BITS != 16 && a.groups > 1;
+        if (k0 + kStep > a.k && k0 + kq * 8 * NF >= a.k) {
+            // (a code is finite whatever its bits, a 16-bit weight need not be)
+            if constexpr (!XL) {
+                const u4 zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int f = 0; f < NF; ++f)
+                        x[c][f] = __builtin_bit_cast(typename N::V8, zero);
+            }
             if constexpr (BITS == 16)
 #pragma unroll
                 for (int r = 0; r < WR; ++r)
@@ -71,7 +76,7 @@ struct RowsTile {
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 part[c] = grouped ? (f4){0, 0, 0, 0} : acc[r][c];
-            steps<0>(r, part);
+            steps<0>(r, part, xl + k0 + kq * 8 * NF);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 acc[r][c] = grouped ? acc[r][c] + scale[r] * part[c] : part[c];
@@ -79,24 +84,37 @@ struct RowsTile {
     }
 
     template <int F>
-    __device__ __forceinline__ void steps(int r, f4 (&part)[NC]) const
+    __device__ __forceinline__ void steps(int r, f4 (&part)[NC], const typename N::T *xl) const
     {
         if constexpr (F < NF) {
             const typename N::V8 b = expand<N, BITS, F>(w[r]);
+            if constexpr (XL) {
+                part[0] = mfma16(*(const typename N::V8 *)(xl + 8 * F), b, part[0]);
+            } else {
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                part[c] = mfma16(x[c][F], b, part[c]);
-            steps<F + 1>(r, part);
+                for (int c = 0; c < NC; ++c)
+                    part[c] = mfma16(x[c][F], b, part[c]);
+            }
+            steps<F + 1>(r, part, xl);
         }
     }
 };
 
-template <class N, int BITS, int NF, int WR, int NC, bool GATED, int WAVES>
+// Bytes of x in local memory.
+template <int NF>
+size_t rows_x_bytes(const MatmulArgs &a)
+{
+    constexpr int64_t step = 32 * NF;
+    return (size_t)a.r * (size_t)(((a.k + step - 1) / step * step + 8) * 2);
+}
+
+template <class N, int BITS, int NF, int WR, int NC, bool GATED, bool XL, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
 {
-    using Tile = RowsTile<N, BITS, NF, WR, NC, GATED>;
+    using Tile = RowsTile<N, BITS, NF, WR, NC, GATED, XL>;
+    static_assert(!XL || NC == 1, "sixteen rows at most");
     constexpr int AHEAD = NC == 1 ? 4 : 2;
-    extern __shared__ f4 part[];  // [wave][WR][NC][64]
+    extern __shared__ f4 part[];  // [wave][WR][NC][64]; before that, XL: x
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int OUT = GATED ? 8 * WR : 16 * WR;  // outputs of a workgroup
@@ -133,17 +151,35 @@ __global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
         load(t[i], first + i);
+    // x (XL): whole rows, zero up to whole steps, a row's pieces off the next one's banks
+    typename N::T *xl = (typename N::T *)part;
+    if constexpr (XL) {
+        const int32_t kp = steps * Tile::kStep, pieces = kp / 8;
+        for (int32_t e = threadIdx.x; e < a.r * pieces; e += 64 * WAVES) {
+            const int32_t r = e / pieces, k = (e - r * pieces) * 8;
+            u4 v = {0, 0, 0, 0};
+            if (k < a.k)
+                v = *(const u4 *)((const typename N::T *)a.x + r * a.x_pitch + k);
+            *(u4 *)(xl + r * (kp + 8) + k) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // (the weights' loads stay in flight)
+        asm volatile("" ::: "memory");
+        xl += min(l16, a.r - 1) * (kp + 8);
+    }
     int32_t s = first;
     for (; last - s > AHEAD; s += AHEAD)
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            t[i].add(acc, a, (s + i) * Tile::kStep, kq);
+            t[i].add(acc, a, (s + i) * Tile::kStep, kq, xl);
             load(t[i], s + i + AHEAD);
         }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
         if (s + i < last)
-            t[i].add(acc, a, (s + i) * Tile::kStep, kq);
+            t[i].add(acc, a, (s + i) * Tile::kStep, kq, xl);
+    if constexpr (XL)
+        __syncthreads();  // x has been read
 #pragma unroll
     for (int r = 0; r < WR; ++r) {
         float unscale = kUnscale<BITS>;
@@ -178,22 +214,42 @@ __global__ void __launch_bounds__(64 * WAVES) matmul_rows_kernel(MatmulArgs a)
     }
 }
 
-template <class N, int BITS, int NF, int WR, int NC, bool GATED, int WAVES>
+template <class N, int BITS, int NF, int WR, int NC, bool GATED, bool XL, int WAVES>
 hipError_t launch_rows(const MatmulArgs &a, hipStream_t s)
 {
     constexpr int OUT = GATED ? 8 * WR : 16 * WR;
     const dim3 grid((a.m + OUT - 1) / OUT, (a.r + 16 * NC - 1) / (16 * NC));
-    hipLaunchKernelGGL((matmul_rows_kernel<N, BITS, NF, WR, NC, GATED, WAVES>), grid, dim3(64 * WAVES),
-                       WAVES * WR * NC * 64 * sizeof(f4), s, a);
+    size_t lds = WAVES * WR * NC * 64 * sizeof(f4);
+    if (XL && lds < rows_x_bytes<NF>(a))
+        lds = rows_x_bytes<NF>(a);
+    hipLaunchKernelGGL((matmul_rows_kernel<N, BITS, NF, WR, NC, GATED, XL, WAVES>), grid, dim3(64 * WAVES), lds, s, a);
     return hipGetLastError();
+}
+
+// Up to 16 rows: x is read from local memory where it fits (32 KB leave room
+// for more workgroups); two blocks of rows of weights a workgroup where that
+// leaves two workgroups for each compute unit.
+template <class N, int BITS, int NF, bool GATED>
+hipError_t launch_rows_few(const MatmulArgs &a, hipStream_t s)
+{
+    const int64_t rows = GATED ? 2 * (int64_t)a.m : a.m;
+    const bool local = rows_x_bytes<NF>(a) <= 32 * 1024;
+    if (GATED || rows >= 32 * 512)
+        return local ? launch_rows<N, BITS, NF, 2, 1, GATED, true, 8>(a, s)
+                     : launch_rows<N, BITS, NF, 2, 1, GATED, false, 8>(a, s);
+    if constexpr (!GATED)
+        return local ? launch_rows<N, BITS, NF, 1, 1, false, true, 8>(a, s)
+                     : launch_rows<N, BITS, NF, 1, 1, false, false, 8>(a, s);
+    return hipErrorInvalidValue;
 }
 
 template <class N, int BITS, int NF>
 hipError_t launch_rows_sized(const MatmulArgs &a, hipStream_t s)
 {
-    if (a.gated)
-        return a.r <= 16 ? launch_rows<N, BITS, NF, 2, 1, true, 8>(a, s) : launch_rows<N, BITS, NF, 2, 4, true, 8>(a, s);
-    return a.r <= 16 ? launch_rows<N, BITS, NF, 1, 1, false, 8>(a, s) : launch_rows<N, BITS, NF, 2, 4, false, 8>(a, s);
+    if (a.r <= 16)
+        return a.gated ? launch_rows_few<N, BITS, NF, true>(a, s) : launch_rows_few<N, BITS, NF, false>(a, s);
+    return a.gated ? launch_rows<N, BITS, NF, 2, 4, true, false, 8>(a, s)
+                   : launch_rows<N, BITS, NF, 2, 4, false, false, 8>(a, s);
 }
 
 // A lane's piece is a quarter of a group at most.
