@@ -128,6 +128,7 @@ CacheArgs cache_args(const qnn_lm_cache *c)
     a.v_page = c->v_page;
     a.v_head = c->v_head;
     a.v_slot = c->v_slot;
+    a.page_div = qnn::make_fastdiv((uint32_t)c->page);
     return a;
 }
 

@@ -47,7 +47,6 @@ struct AttendPlan {
     int32_t nr;         // sixteens of rows of a wave
     int32_t row_tiles;  // of 16 nr rows, or of 64 nr
     int32_t splits;     // pieces of the positions
-    int32_t shift;      // page = 1 << shift, or -1
     float *part;        // [splits][b][t][heads][dim] outputs, then their maxima and sums
 };
 

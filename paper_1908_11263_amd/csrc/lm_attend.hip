@@ -60,10 +60,6 @@ static AttendPlan plan_attend(const AttendArgs &a, const CacheArgs &c, int dim)
     int64_t splits = (512 + groups - 1) / groups;
     splits = splits < most ? splits : most;
     p.splits = (int32_t)(splits < 1 ? 1 : splits);
-    p.shift = -1;
-    for (int i = 0; i < 31; ++i)
-        if (c.page == 1 << i)
-            p.shift = i;
     p.part = nullptr;
     return p;
 }

@@ -39,24 +39,24 @@ struct KvTile {
 
     // Page of position lane % 32 as the table says; looked at in load(), a tile
     // later (loads come back in order: a comparison here would wait for all).
-    static __device__ __forceinline__ int32_t look(const CacheArgs &c, int shift, int32_t seq, int32_t p0, int32_t end,
+    static __device__ __forceinline__ int32_t look(const CacheArgs &c, int32_t seq, int32_t p0, int32_t end,
                                                    int lane)
     {
         const int32_t pos = max(min(p0 + (lane & 31), end - 1), 0);
-        const int32_t pg = shift >= 0 ? pos >> shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
+        const int32_t pg = qnn::fdiv((uint32_t)pos, c.page_div);
         return c.table[(int64_t)seq * c.width + pg];
     }
 
     // Loads are never skipped (behind a branch that may skip one, a wait for an
     // older load has to be a wait for all): what is not there is read from slot
     // 0 of page 0, and masked or cleared later.
-    __device__ __forceinline__ void load(const CacheArgs &c, int shift, int32_t page, int32_t head, int32_t p0,
+    __device__ __forceinline__ void load(const CacheArgs &c, int32_t page, int32_t head, int32_t p0,
                                          int32_t end, int lane)
     {
         const int32_t pos = p0 + (lane & 31);
         const bool there = pos < end && (uint32_t)page < (uint32_t)c.pages;
         valid = (uint32_t)__ballot(there);
-        int32_t slot = shift >= 0 ? pos & ((1 << shift) - 1) : (int32_t)((uint32_t)pos % (uint32_t)c.page);
+        int32_t slot = pos - (int32_t)qnn::fdiv((uint32_t)pos, c.page_div) * c.page;
         page = there ? page : 0;
         slot = there ? slot : 0;
         if constexpr (BITS != 16) {
@@ -226,10 +226,10 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
     const int32_t share = (tiles + pl.splits - 1) / pl.splits;
     const int32_t first = split * share + wave, last = min((split + 1) * share, tiles);
     using Tile = KvTile<BITS, DIM>;
-    auto look = [&](int32_t t) { return Tile::look(c, pl.shift, seq, t * kAttendTile, end, lane); };
+    auto look = [&](int32_t t) { return Tile::look(c, seq, t * kAttendTile, end, lane); };
     // (tiles past the last are loaded too, from slot 0 of page 0, and not used)
     auto load = [&](Tile &h, int32_t t, int32_t page) {
-        h.load(c, pl.shift, page, head, t * kAttendTile, t < last ? end : 0, lane);
+        h.load(c, page, head, t * kAttendTile, t < last ? end : 0, lane);
     };
     Tile ahead[2];
     const int32_t early[2] = {look(first), look(first + 4)};

@@ -3,7 +3,6 @@
 
 #include "lm_attend_few.h"
 #include "lm_attend_many.h"
-#include "qnn_internal.h"
 
 namespace qnn_lm {
 

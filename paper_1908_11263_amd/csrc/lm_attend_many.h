@@ -119,14 +119,14 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
     // before load(): a comparison would wait for it here.
     auto find = [&](int32_t t, int32_t r) {
         const int32_t pos = max(min(t * KT + r, end - 1), 0);
-        const int32_t pg = pl.shift >= 0 ? pos >> pl.shift : (int32_t)((uint32_t)pos / (uint32_t)c.page);
+        const int32_t pg = qnn::fdiv((uint32_t)pos, c.page_div);
         return c.table[(int64_t)seq * c.width + pg];
     };
     auto in_cache = [&](int32_t t, int32_t r, int32_t page) {
         return t < last && r < KT && t * KT + r < end && (uint32_t)page < (uint32_t)c.pages;
     };
     auto slot_of = [&](int32_t pos) {
-        return pl.shift >= 0 ? pos & ((1 << pl.shift) - 1) : (int32_t)((uint32_t)pos % (uint32_t)c.page);
+        return pos - (int32_t)qnn::fdiv((uint32_t)pos, c.page_div) * c.page;
     };
     // A tile's pages: of position `lane`, and of the positions that this thread loads
     struct Pages {

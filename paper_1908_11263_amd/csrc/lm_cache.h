@@ -17,7 +17,7 @@ __device__ __forceinline__ Slot find_slot(const CacheArgs &c, int32_t seq, int64
     Slot s = {-1, 0};
     if (pos < 0 || pos >= (int64_t)c.width * c.page)
         return s;
-    const int32_t p = (uint32_t)pos / (uint32_t)c.page;  // width * page < 2^31
+    const int32_t p = qnn::fdiv((uint32_t)pos, c.page_div);  // width * page < 2^31
     const int32_t page = c.table[(int64_t)seq * c.width + p];
     if ((uint32_t)page < (uint32_t)c.pages) {
         s.page = page;

@@ -11,6 +11,7 @@ struct TokenArgs {
     int64_t ks[3], vs[3];  // elements: sequence, token, head
     int32_t t;
     uint32_t tokens;       // b * t * 2 * heads
+    qnn::FastDiv heads_div, t_div;
     const int32_t *lens, *counts;
 };
 
@@ -19,15 +20,14 @@ struct TokenArgs {
 struct Token {
     int32_t seq, i, which, head;
 };
-__device__ __forceinline__ Token token_of(uint32_t n, int32_t heads, int32_t t)
+__device__ __forceinline__ Token token_of(uint32_t n, const qnn::FastDiv &heads, const qnn::FastDiv &t)
 {
     Token o;
-    o.head = n % heads;
-    n /= heads;
-    o.which = n & 1;
-    n >>= 1;
-    o.i = n % t;
-    o.seq = n / t;
+    const uint32_t a = qnn::fdiv(n, heads), b = a >> 1;
+    o.head = n - a * heads.d;
+    o.which = a & 1;
+    o.seq = qnn::fdiv(b, t);
+    o.i = b - o.seq * t.d;
     return o;
 }
 
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) append_kernel(CacheArgs c, TokenArgs a)
     const int lane = threadIdx.x % LANES;
     if (n >= a.tokens)
         return;
-    const Token o = token_of(n, c.heads, a.t);
+    const Token o = token_of(n, a.heads_div, a.t_div);
     if (a.counts && o.i >= a.counts[o.seq])
         return;
     const Slot s = find_slot(c, o.seq, (int64_t)a.lens[o.seq] + o.i);
@@ -66,12 +66,27 @@ __global__ void __launch_bounds__(256) append_kernel(CacheArgs c, TokenArgs a)
         constexpr float most = BITS == 8 ? 127.f : 7.f;
         const bool finite = top < 0x7F800000u;
         const float scale = finite ? __uint_as_float(top) / most : __uint_as_float(0x7FC00000u);
+        // v / scale, correctly rounded: with the correctly rounded reciprocal y,
+        // q = v y is within a unit, and q + (v - q scale) y rounds as the quotient
+        // does (Markstein), three operations for each of a token's numbers.
+        // Scales whose reciprocal is not a normal number divide.
         uint32_t code[8];
+        const bool normal = scale >= 0x1p-100f;
+        const float y = normal ? 1.f / scale : 0.f;
+        if (__any(finite && scale > 0.f && !normal)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float q = finite && scale > 0.f ? rintf(v[e] / scale) : 0.f;
-            code[e] = (uint32_t)(int32_t)fminf(fmaxf(q, -most), most);
+            for (int e = 0; e < 8; ++e)
+                v[e] = finite && scale > 0.f ? v[e] / scale : 0.f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float q = v[e] * y;
+                v[e] = finite ? __builtin_fmaf(__builtin_fmaf(-q, scale, v[e]), y, q) : 0.f;
+            }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            code[e] = (uint32_t)(int32_t)fminf(fmaxf(rintf(v[e]), -most), most);
         if constexpr (BITS == 8) {
             u2 r;
             r.x = (code[0] & 255) | (code[1] & 255) << 8 | (code[2] & 255) << 16 | code[3] << 24;
@@ -93,6 +108,7 @@ struct ReadArgs {
     void *k, *v;
     int32_t t;
     uint32_t tokens;          // b * t * 2 * heads
+    qnn::FastDiv heads_div, t_div;
     const int32_t *start;
 };
 
@@ -105,7 +121,7 @@ __global__ void __launch_bounds__(256) read_kernel(CacheArgs c, ReadArgs a)
     const int lane = threadIdx.x % LANES;
     if (n >= a.tokens)
         return;
-    const Token o = token_of(n, c.heads, a.t);
+    const Token o = token_of(n, a.heads_div, a.t_div);
     void *dst = o.which ? a.v : a.k;
     if (!dst)
         return;
@@ -211,6 +227,8 @@ hipError_t launch_append(const CacheArgs &c, int bits, int dim, int type, const 
     }
     a.t = t;
     a.tokens = (uint32_t)((int64_t)c.b * t * 2 * c.heads);
+    a.heads_div = qnn::make_fastdiv((uint32_t)c.heads);
+    a.t_div = qnn::make_fastdiv((uint32_t)t);
     a.lens = lens;
     a.counts = counts;
     if (bits == 16)
@@ -248,6 +266,8 @@ hipError_t launch_read(const CacheArgs &c, int bits, int dim, int type, int cach
     a.v = v;
     a.t = t;
     a.tokens = (uint32_t)((int64_t)c.b * t * 2 * c.heads);
+    a.heads_div = qnn::make_fastdiv((uint32_t)c.heads);
+    a.t_div = qnn::make_fastdiv((uint32_t)t);
     a.start = start;
     if (type == QNN_LM_F32)
         return read_typed<F32>(c, bits, dim, cache_type, a, s);

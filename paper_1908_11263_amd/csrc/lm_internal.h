@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "qnn_internal.h"
 #include "qnn_lm.h"
 
 namespace qnn_lm {
@@ -43,6 +44,7 @@ struct CacheArgs {
     const int32_t *table;
     int32_t pages, heads, page, b, width;
     int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
+    qnn::FastDiv page_div;
 };
 hipError_t launch_append(const CacheArgs &c, int bits, int dim, int type, const void *k, const void *v,
                          const int64_t *k_stride, const int64_t *v_stride, int t, const int32_t *lens,

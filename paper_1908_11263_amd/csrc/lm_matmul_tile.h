@@ -22,7 +22,6 @@
 #pragma once
 
 #include "lm_matmul.h"
-#include "qnn_internal.h"
 
 namespace qnn_lm {
 

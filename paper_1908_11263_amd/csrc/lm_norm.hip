@@ -176,7 +176,9 @@ hipError_t launch_sized(const NormArgs &a, hipStream_t s)
     }
     if constexpr (VEC == 8) {
         QNN_LM_NORM(1, 2)
+        QNN_LM_NORM(4, 1)
         QNN_LM_NORM(4, 2)
+        QNN_LM_NORM(4, 3)
         QNN_LM_NORM(4, 4)
         QNN_LM_NORM(16, 4)
     } else {
