@@ -21,9 +21,11 @@
  * Arithmetic.  Products are exact (a code is an exact 16-bit number), sums,
  * softmax statistics, norms and epilogues are kept in 32-bit floating point;
  * results are rounded once, to nearest even, when they are stored.  The
- * attention's probabilities are rounded to the queries' type before they
- * multiply the values, their sum is not.  The order of every sum is fixed: the
- * same call gives the same bits.
+ * attention's probabilities multiply the values as 16-bit numbers, each off by
+ * 2^-12 of itself at most (2^-9 over a cache of bf16 numbers); with up to 32 rows
+ * a cache head (16 of 256 channels) as the sum of two such numbers.  Their own
+ * sum is not rounded.  The order of every sum is fixed: the same call gives the
+ * same bits.
  * Values that live on the device (lengths, page numbers, paths) cannot be
  * checked on the host.  The kernels bound every index that they make of them:
  * a position whose page number is outside of the cache, or that the table does

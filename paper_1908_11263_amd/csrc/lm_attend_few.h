@@ -304,7 +304,9 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                         s[n][u][i] = (see >> (16 * u + i)) & 1 ? s[n][u][i] : -INFINITY;
             }
         }
-        typename P::V8 p[NR];
+        // (two 16-bit numbers a probability, as few rows leave room for: their
+        // rounding does not show in the result)
+        typename P::V8 p[NR], rest[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
@@ -339,6 +341,11 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             }
             const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
             p[n] = __builtin_bit_cast(typename P::V8, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                e[i] -= (float)p[n][i];
+            const u4 r2 = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
+            rest[n] = __builtin_bit_cast(typename P::V8, r2);
         }
         if (!odd) {
 #pragma unroll
@@ -346,7 +353,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                 const typename P::V8 vf = value_frag<P, BITS, DIM>(vl, d, lane);
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
-                    o[n][d] = mfma16(vf, p[n], o[n][d]);
+                    o[n][d] = mfma16(vf, rest[n], mfma16(vf, p[n], o[n][d]));
             }
         } else if constexpr (BITS == 16) {
 #pragma unroll
