@@ -292,13 +292,14 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         unit[n] = 1.f, clear[n] = 0;
 
     const int32_t begin = split * g.steps, steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
-    float f[WF];  // old unit over new, of the group that begins
-#pragma unroll
-    for (int n = 0; n < WF; ++n)
-        f[n] = 1.f;
     constexpr int BLOCKS = S::KS / 32;
+    float f[BLOCKS][WF];  // old unit over new, of the group that begins with a block
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int n = 0; n < WF; ++n)
+            f[b][n] = 1.f;
     Raw<BITS, WF> raw[BLOCKS];
-    Eight<N, TF, WF> pair[2];
     auto read_raw = [&](const uint8_t *ws) {
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
@@ -337,18 +338,18 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 const float ratio = k == begin * S::KS ? 0.f : unit[n] / sc;
                 const bool zero = sc == 0.f || __builtin_isinf(ratio);
                 clear[n] = zero ? 0xFFFFFFFFu : 0;
-                f[n] = zero || k == begin * S::KS ? 1.f : ratio;
+                f[b][n] = zero || k == begin * S::KS ? 1.f : ratio;
                 unit[n] = zero ? unit[n] : sc;
             }
             return true;
         }
     };
-    auto rescale = [&] {
+    auto rescale = [&](int b) {
 #pragma unroll
         for (int m = 0; m < TF; ++m)
 #pragma unroll
             for (int n = 0; n < WF; ++n)
-                acc[m][n] *= f[n];
+                acc[m][n] *= f[b][n];
     };
     // (no branch between an eight's products and the next one's preparation:
     // they are to alternate)
@@ -364,48 +365,130 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     __builtin_amdgcn_s_barrier();
     issue(min(begin + S::kStages - 1, steps - 1), S::kStages - 1);
     int buf = 0;
-    read_raw(lds + S::kXBytes);
-    bool scale = begins(begin, 0, lds + S::kXBytes);
-    fetch<N, BITS, TF, WF, GPB, 0>(lds, raw[0], clear, 0, l32, half, pair[0]);
     // (k is a multiple of 32: the last step of all may be one block)
     const bool half_step = BLOCKS == 2 && steps * S::KS > a.k;
     const int32_t whole = half_step ? steps - 1 : steps;
-    for (int32_t s = begin; s < whole; ++s) {
-        const uint8_t *xs = lds + buf * S::kStage;
-        if (GPB && scale)
-            rescale();
-        fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
-        multiply(pair[0]);
-        if constexpr (BLOCKS == 2) {
-            if constexpr (GPB == 2)
-                begins(s, 1, xs + S::kXBytes);
-            fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, pair[0]);
-            multiply(pair[1]);
-            if constexpr (GPB == 2)
-                rescale();
-            fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[1], clear, 1, l32, half, pair[1]);
+    if constexpr (TF == 4) {
+        // an eight ahead
+        Eight<N, TF, WF> pair[2];
+        read_raw(lds + S::kXBytes);
+        bool scale = begins(begin, 0, lds + S::kXBytes);
+        fetch<N, BITS, TF, WF, GPB, 0>(lds, raw[0], clear, 0, l32, half, pair[0]);
+        for (int32_t s = begin; s < whole; ++s) {
+            const uint8_t *xs = lds + buf * S::kStage;
+            if (GPB && scale)
+                rescale(0);
+            fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
             multiply(pair[0]);
+            if constexpr (BLOCKS == 2) {
+                if constexpr (GPB == 2)
+                    begins(s, 1, xs + S::kXBytes);
+                fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, pair[0]);
+                multiply(pair[1]);
+                if constexpr (GPB == 2)
+                    rescale(1);
+                fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[1], clear, 1, l32, half, pair[1]);
+                multiply(pair[0]);
+            }
+            // Everything of this step has been read: the next one's copies are
+            // waited for, and this one's place is filled again (past the last step
+            // with the last one, so that the counts stay).
+            wait_copies<(S::kStages - 2) * S::kCopies>();
+            __builtin_amdgcn_s_barrier();
+            issue(min(s + S::kStages, steps - 1), buf);
+            buf = buf == S::kStages - 1 ? 0 : buf + 1;
+            const uint8_t *xn = lds + buf * S::kStage;
+            read_raw(xn + S::kXBytes);
+            scale = s + 1 < steps && begins(s + 1, 0, xn + S::kXBytes);
+            fetch<N, BITS, TF, WF, GPB, 0>(xn, raw[0], clear, 0, l32, half, pair[0]);
+            multiply(pair[1]);
         }
-        // Everything of this step has been read: the next one's copies are
-        // waited for, and this one's place is filled again (past the last step
-        // with the last one, so that the counts stay).
-        wait_copies<(S::kStages - 2) * S::kCopies>();
-        __builtin_amdgcn_s_barrier();
-        issue(min(s + S::kStages, steps - 1), buf);
-        buf = buf == S::kStages - 1 ? 0 : buf + 1;
-        const uint8_t *xn = lds + buf * S::kStage;
-        read_raw(xn + S::kXBytes);
-        scale = s + 1 < steps && begins(s + 1, 0, xn + S::kXBytes);
-        fetch<N, BITS, TF, WF, GPB, 0>(xn, raw[0], clear, 0, l32, half, pair[0]);
-        multiply(pair[1]);
-    }
-    if (half_step) {
-        const uint8_t *xs = lds + buf * S::kStage;
-        if (GPB && scale)
-            rescale();
-        fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
-        multiply(pair[0]);
-        multiply(pair[1]);
+        if (half_step) {
+            const uint8_t *xs = lds + buf * S::kStage;
+            if (GPB && scale)
+                rescale(0);
+            fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
+            multiply(pair[0]);
+            multiply(pair[1]);
+        }
+    } else {
+        // Smaller tiles have too few products in an eight to cover local
+        // memory's answers, and the registers for whole steps: a step ahead.
+        Eight<N, TF, WF> ahead[2][2 * BLOCKS];
+        bool scale[2] = {false, false};  // a group begins with the step
+        auto prepare = [&](int32_t s, Eight<N, TF, WF> (&to)[2 * BLOCKS], bool &first) {
+            const uint8_t *xs = lds + buf * S::kStage;
+            read_raw(xs + S::kXBytes);
+            first = s < steps && begins(s, 0, xs + S::kXBytes);
+            fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[0], clear, 0, l32, half, to[0]);
+            fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, to[1]);
+            if constexpr (BLOCKS == 2) {
+                if constexpr (GPB == 2)
+                    if (s < whole)
+                        begins(s, 1, xs + S::kXBytes);
+                fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, to[2]);
+                fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[1], clear, 1, l32, half, to[3]);
+            }
+        };
+        // The scales of step s + 1 are read while step s is multiplied: what
+        // step s is brought to has been put aside.
+        float g[BLOCKS][WF];
+        auto set_aside = [&] {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int n = 0; n < WF; ++n)
+                    g[b][n] = f[b][n];
+        };
+        auto bring = [&](int b) {
+#pragma unroll
+            for (int m = 0; m < TF; ++m)
+#pragma unroll
+                for (int n = 0; n < WF; ++n)
+                    acc[m][n] *= g[b][n];
+        };
+        auto step = [&](int32_t s, const Eight<N, TF, WF> (&cur)[2 * BLOCKS], bool first, Eight<N, TF, WF> (&next)[2 * BLOCKS],
+                        bool &next_first) {
+            if constexpr (GPB)
+                set_aside();
+            // Step s has been read: its place is filled again (past the last
+            // step with the last one, so that the counts stay).
+            wait_copies<(S::kStages - 2) * S::kCopies>();
+            __builtin_amdgcn_s_barrier();
+            issue(min(s + S::kStages, steps - 1), buf);
+            buf = buf == S::kStages - 1 ? 0 : buf + 1;
+            prepare(s + 1, next, next_first);
+            if (GPB && first)
+                bring(0);
+            products<N, TF, WF>(cur[0], acc);
+            products<N, TF, WF>(cur[1], acc);
+            if constexpr (BLOCKS == 2) {
+                if constexpr (GPB == 2)
+                    bring(1);
+                products<N, TF, WF>(cur[2], acc);
+                products<N, TF, WF>(cur[3], acc);
+            }
+        };
+        prepare(begin, ahead[0], scale[0]);
+        int32_t s = begin;
+        for (; s + 1 < whole; s += 2) {
+            step(s, ahead[0], scale[0], ahead[1], scale[1]);
+            step(s + 1, ahead[1], scale[1], ahead[0], scale[0]);
+        }
+        const bool odd = s < whole;
+        if (odd)
+            step(s, ahead[0], scale[0], ahead[1], scale[1]);
+        if (half_step) {
+            if (GPB && (odd ? scale[1] : scale[0]))
+                rescale(0);
+            if (odd) {
+                products<N, TF, WF>(ahead[1][0], acc);
+                products<N, TF, WF>(ahead[1][1], acc);
+            } else {
+                products<N, TF, WF>(ahead[0][0], acc);
+                products<N, TF, WF>(ahead[0][1], acc);
+            }
+        }
     }
     // the copies of the last steps, made again, are there before local memory
     // is used anew
