@@ -48,7 +48,9 @@ TilePlan plan_matmul(const MatmulArgs &a, int bits)
 {
     TilePlan p = {0, 0, 1, (a.k + 127) / 128 * 128};
     // (the tile kernel's offsets within a tile are 32 bits)
-    if (a.r <= 16 || a.x_pitch >= 1 << 23 || a.w_row >= 1 << 23)
+    // (and it copies four scales at a time)
+    if (a.r <= 16 || a.x_pitch >= 1 << 23 || a.w_row >= 1 << 23 ||
+        (a.groups > 1 && (a.gated ? 2 : 1) * (int64_t)a.m * a.groups < 4))
         return p;
     const int64_t rows = a.gated ? 2 * (int64_t)a.m : a.m;
     const bool near = rows * a.w_row < (int64_t)1 << 31;  // a gated tile of 128 rows reaches both halves

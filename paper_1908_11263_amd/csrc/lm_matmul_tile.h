@@ -71,14 +71,20 @@ struct TileShape {
     static constexpr int kWUnits = kWRow / kWUnit;     // of a row
     static constexpr int kXCopies = BM * kXRow / 1024 / 4;         // instructions of a wave a step
     static constexpr int kWCopies = BN * kWUnits / 64 / 4;
-    static constexpr int kCopies = kXCopies + kWCopies + GPB;
+    static constexpr int kCopies = kXCopies + kWCopies;  // (now and then one of scales besides)
     static constexpr int kXBytes = BM * kXRow, kWBytes = BN * kWRow;
-    static constexpr int kStage = kXBytes + kWBytes + GPB * BN * 4;
+    static constexpr int kStage = kXBytes + kWBytes;
+    // Scales come four groups at a time, 16 bytes a row (one at a time they
+    // would be as many requests as x and the codes together).  A place is used
+    // again when the copies ahead can no longer need it.
+    static constexpr int kScaleRing = GPB == 2 ? 3 : 2, kScaleSteps = GPB == 2 ? 2 : 4;  // steps of four groups, at least
+    static constexpr int kScales = GPB ? kScaleRing * BN * 16 : 0;
     // two workgroups a compute unit
-    static constexpr int kStages = 4 * kStage <= 64 * 1024 ? 4 : 3 * kStage <= 80 * 1024 ? 3 : 2;
+    static constexpr int kStages = 4 * kStage + kScales <= 64 * 1024 ? 4 : 3 * kStage + kScales <= 80 * 1024 ? 3 : 2;
+    static_assert(!GPB || kStages <= (kScaleRing - 1) * kScaleSteps, "scales are overwritten too early");
     static constexpr int kOutPitch = BN + 4;                  // floats
     static constexpr int kOut = 32 * kOutPitch * 4;
-    static constexpr int kLds = kStages * kStage > kOut ? kStages * kStage : kOut;
+    static constexpr int kLds = kStages * kStage + kScales > kOut ? kStages * kStage + kScales : kOut;
 
     // Place of piece c of row r among the row's pieces: 256 bytes of local memory
     // answer at once, so the pieces that sixteen neighbouring lanes read, one a
@@ -224,29 +230,37 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
             wo[i] = (uint32_t)(min(j0 + r, a.m - 1) - j0) * (uint32_t)a.w_row + wc[i] * S::kWUnit;
         }
     }
-    // scales: one a lane and group (gated: all of a half, then the other's)
+    // Scales: four of a row a lane (gated: a half's rows, then the other's).  A
+    // row's last four may lie before its place, so that nothing is read past
+    // the end of all.
+    const int32_t begin = split * g.steps;  // first step
+    const int gshift = GPB ? __builtin_ctz(a.group) : 0;
+    const int64_t most = (GATED ? 2 * (int64_t)a.m : a.m) * a.groups - 4;  // last place of four
     const float *sb = nullptr;
-    uint32_t so = 0;
+    int64_t sfirst = 0, srow = 0;  // elements: of sb, of this lane's row
     if constexpr (GPB) {
         const int e = (WF == 2 ? wave : wave & 1) * 64 + lane;
         const int up = GATED ? e / (S::BN / 2) : 0, j = GATED ? e % (S::BN / 2) : e;
-        sb = a.scale + (int64_t)j0 * a.groups;
-        if constexpr (GATED) {
-            if constexpr (WF == 2) {
-                sb += (int64_t)(wave >> 1) * a.m * a.groups;
-                so = (uint32_t)(min(j0 + j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
-            } else {
-                so = (uint32_t)(up * a.m + min(j0 + j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
-            }
-        } else {
-            so = (uint32_t)(min(j0 + j, a.m - 1) - j0) * (uint32_t)(a.groups * 4);
-        }
+        srow = ((int64_t)up * a.m + min(j0 + j, a.m - 1)) * a.groups;
+        sfirst = ((int64_t)(GATED && WF == 2 ? wave >> 1 : 0) * a.m + j0) * a.groups - 4;
+        sfirst = sfirst < 0 ? 0 : sfirst;
+        sb = a.scale + sfirst;
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
     auto issue = [&](int32_t step, int buf) {
         const int32_t k0 = step * S::KS, left = a.k - k0;  // a multiple of 32
         const uint32_t at = lds0 + buf * S::kStage;
+        if constexpr (GPB) {
+            // before the step's other copies: those are counted, this one is not
+            const int32_t quad = k0 >> gshift >> 2;
+            if (step == begin || (k0 & ((4 << gshift) - 1)) == 0) {
+                const int64_t e = srow + 4 * quad < most ? srow + 4 * quad : most;
+                copy_to_lds<16>(sb, (uint32_t)(e - sfirst) * 4,
+                                lds0 + S::kStages * S::kStage + quad % S::kScaleRing * (S::BN * 16) +
+                                    (WF == 2 ? wave : wave & 1) * 1024);
+            }
+        }
         const uint8_t *x = xb + (int64_t)k0 * 2;
         const int64_t w = (int64_t)k0 * BITS / 8;
         const uint32_t xat = at + wave * S::kXCopies * 1024,
@@ -268,13 +282,6 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 copy_to_lds<S::kWUnit>(wb[i] + w, wc[i] * (S::kWUnit * 8 / BITS) < left ? wo[i] : wo[i] - wc[i] * S::kWUnit,
                                        wat + i * 64 * S::kWUnit);
         }
-        if constexpr (GPB) {
-            const int32_t grp = k0 >> __builtin_ctz(a.group);
-#pragma unroll
-            for (int i = 0; i < GPB; ++i)
-                copy_to_lds<4>(sb + min(grp + i, a.groups - 1), so,
-                               at + S::kXBytes + S::kWBytes + (i * S::BN + (WF == 2 ? wave : wave & 1) * 64) * 4);
-        }
     };
 
     f16v acc[TF][WF];
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     for (int n = 0; n < WF; ++n)
         unit[n] = 1.f, clear[n] = 0;
 
-    const int32_t begin = split * g.steps, steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
+    const int32_t steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
     constexpr int BLOCKS = S::KS / 32;
     float f[BLOCKS][WF];  // old unit over new, of the group that begins with a block
 #pragma unroll
@@ -321,20 +328,30 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 }
             }
     };
+    // Scales from a row's first to the last place of four.
+    int32_t sleft[WF];
+#pragma unroll
+    for (int n = 0; n < WF; ++n) {
+        const int q = n * 32 + l32;  // row of this wave
+        const int32_t j = min(j0 + (GATED ? wave * GR + q % HR : wave * WF * 32 + q), a.m - 1);
+        const int64_t left = most - ((GATED && q >= GR ? (int64_t)a.m : 0) + j) * a.groups;
+        sleft[n] = (int32_t)(left < 1 << 30 ? left : 1 << 30);
+    }
     // Whether block b of step s begins a group; if so its scale is the new unit.
-    auto begins = [&](int32_t s, int b, const uint8_t *ws) {
+    auto begins = [&](int32_t s, int b) {
         if constexpr (!GPB) {
             return false;
         } else {
             const int32_t k = s * S::KS + b * 32;
             if (k & (a.group - 1))
                 return false;
-            const float *ss = (const float *)(ws + S::kWBytes);
+            const int32_t group = k >> gshift, quad = group >> 2;
+            const float *ss = (const float *)(lds + S::kStages * S::kStage + quad % S::kScaleRing * (S::BN * 16));
 #pragma unroll
             for (int n = 0; n < WF; ++n) {
                 const int at = !GATED ? (wave * WF + n) * 32 + l32
                                : WF == 2 ? n * 128 + wave * 32 + l32 : (l32 >> 4) * 64 + wave * 16 + (l32 & 15);
-                const float sc = ss[(GPB == 2 ? b * S::BN : 0) + at];
+                const float sc = ss[at * 4 + (group & 3) + max(0, 4 * quad - sleft[n])];
                 const float ratio = k == begin * S::KS ? 0.f : unit[n] / sc;
                 const bool zero = sc == 0.f || __builtin_isinf(ratio);
                 clear[n] = zero ? 0xFFFFFFFFu : 0;
@@ -372,7 +389,7 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         // an eight ahead
         Eight<N, TF, WF> pair[2];
         read_raw(lds + S::kXBytes);
-        bool scale = begins(begin, 0, lds + S::kXBytes);
+        bool scale = begins(begin, 0);
         fetch<N, BITS, TF, WF, GPB, 0>(lds, raw[0], clear, 0, l32, half, pair[0]);
         for (int32_t s = begin; s < whole; ++s) {
             const uint8_t *xs = lds + buf * S::kStage;
@@ -382,7 +399,7 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
             multiply(pair[0]);
             if constexpr (BLOCKS == 2) {
                 if constexpr (GPB == 2)
-                    begins(s, 1, xs + S::kXBytes);
+                    begins(s, 1);
                 fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, pair[0]);
                 multiply(pair[1]);
                 if constexpr (GPB == 2)
@@ -399,7 +416,7 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
             buf = buf == S::kStages - 1 ? 0 : buf + 1;
             const uint8_t *xn = lds + buf * S::kStage;
             read_raw(xn + S::kXBytes);
-            scale = s + 1 < steps && begins(s + 1, 0, xn + S::kXBytes);
+            scale = s + 1 < steps && begins(s + 1, 0);
             fetch<N, BITS, TF, WF, GPB, 0>(xn, raw[0], clear, 0, l32, half, pair[0]);
             multiply(pair[1]);
         }
@@ -419,13 +436,13 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         auto prepare = [&](int32_t s, Eight<N, TF, WF> (&to)[2 * BLOCKS], bool &first) {
             const uint8_t *xs = lds + buf * S::kStage;
             read_raw(xs + S::kXBytes);
-            first = s < steps && begins(s, 0, xs + S::kXBytes);
+            first = s < steps && begins(s, 0);
             fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[0], clear, 0, l32, half, to[0]);
             fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, to[1]);
             if constexpr (BLOCKS == 2) {
                 if constexpr (GPB == 2)
                     if (s < whole)
-                        begins(s, 1, xs + S::kXBytes);
+                        begins(s, 1);
                 fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, to[2]);
                 fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[1], clear, 1, l32, half, to[3]);
             }
