@@ -3,41 +3,71 @@
 
 namespace qnn_lm {
 
-// One wave a row of outputs.
+constexpr int kMostSplits = 512;
+
+// Joins the pieces of a row's positions: a workgroup a row.  The pieces' maxima
+// are read at once and turned into factors; then DIM / 4 threads own four
+// channels each of every (1024 / DIM)-th piece (their loads do not wait for each
+// other), and the sums of those are added in order.
 template <class N, int DIM>
 __global__ void __launch_bounds__(256) join_kernel(const float *part, void *out, float *lse, int64_t all, int32_t splits)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= all)
-        return;
+    constexpr int LANES = DIM / 4, SETS = 256 / LANES;
+    __shared__ float factor[kMostSplits], red[8];
+    __shared__ f4 sums[SETS][LANES];
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float *ml = part + splits * all * DIM;
-    float m = -INFINITY;
-    for (int s = lane; s < splits; s += 64)
-        m = fmaxf(m, ml[(s * all + row) * 2]);
+    float m[2], l[2], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int s = i * 256 + tid;
+        m[i] = s < splits ? ml[(s * all + row) * 2] : -INFINITY;
+        l[i] = s < splits ? ml[(s * all + row) * 2 + 1] : 0.f;
+        top = fmaxf(top, m[i]);
+    }
 #pragma unroll
     for (int o = 32; o; o >>= 1)
-        m = fmaxf(m, __shfl_xor(m, o, 64));
-    constexpr int E = DIM / 64;
-    float l = 0.f, v[E] = {};
-    if (m != -INFINITY)
-        for (int s = 0; s < splits; ++s) {
-            const int64_t at = s * all + row;
-            const float ms = ml[at * 2];
-            if (ms == -INFINITY)
-                continue;
-            const float f = __builtin_amdgcn_exp2f(ms - m);
-            l += ml[at * 2 + 1] * f;
+        top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (lane == 0)
+        red[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                v[e] += part[at * DIM + lane * E + e] * f;
-        }
-    const float inv = m == -INFINITY ? 0.f : 1.f / l;
+    for (int i = 0; i < 2; ++i) {
+        const int s = i * 256 + tid;
+        // (a piece that has seen nothing counts for nothing, whatever it holds)
+        const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
+        if (s < splits)
+            factor[s] = f;
+        sum += m[i] == -INFINITY ? 0.f : l[i] * f;
+    }
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        store1<N>(out, row * DIM + lane * E + e, v[e] * inv);
-    if (lse && lane == 0)
-        lse[row] = m == -INFINITY ? -INFINITY : 0.693147180559945f * (m + log2f(l));
+    for (int o = 32; o; o >>= 1)
+        sum += __shfl_xor(sum, o, 64);
+    if (lane == 0)
+        red[4 + wave] = sum;
+    __syncthreads();
+    sum = (red[4] + red[5]) + (red[6] + red[7]);
+    const int c = tid % LANES, set = tid / LANES;
+    f4 v = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = set; s < splits; s += SETS)
+        v += *(const f4 *)(part + (s * all + row) * DIM + 4 * c) * factor[s];
+    sums[set][c] = v;
+    __syncthreads();
+    if (tid < LANES) {
+        v = sums[0][c];
+#pragma unroll
+        for (int i = 1; i < SETS; ++i)
+            v += sums[i][c];
+        const float inv = top == -INFINITY ? 0.f : 1.f / sum;
+        const u2 r = {pack2<N>(v[0] * inv, v[1] * inv), pack2<N>(v[2] * inv, v[3] * inv)};
+        *(u2 *)((typename N::T *)out + row * DIM + 4 * c) = r;
+    }
+    if (lse && tid == 0)
+        lse[row] = top == -INFINITY ? -INFINITY : 0.693147180559945f * (top + log2f(sum));
 }
 
 // Rows a workgroup and pieces of the positions.  Up to 32 rows (16 of 256
@@ -57,8 +87,8 @@ static AttendPlan plan_attend(const AttendArgs &a, const CacheArgs &c, int dim)
     p.row_tiles = (p.rows + tile - 1) / tile;
     const int64_t groups = (int64_t)p.row_tiles * c.heads * c.b;
     const int64_t most = ((int64_t)c.width * c.page + 127) / 128;
-    int64_t splits = (512 + groups - 1) / groups;
-    splits = splits < most ? splits : most;
+    int64_t splits = (kMostSplits + groups - 1) / groups;
+    splits = splits < most ? splits : most;  // (at most kMostSplits)
     p.splits = (int32_t)(splits < 1 ? 1 : splits);
     p.part = nullptr;
     return p;
@@ -75,7 +105,7 @@ size_t attend_workspace(const AttendArgs &a, const CacheArgs &c, int dim)
 template <class N>
 static hipError_t launch_join(const AttendArgs &a, const AttendPlan &p, int64_t all, int dim, hipStream_t s)
 {
-    const dim3 grid((unsigned)((all + 3) / 4));
+    const dim3 grid((unsigned)all);
     if (dim == 64)
         hipLaunchKernelGGL((join_kernel<N, 64>), grid, dim3(256), 0, s, p.part, a.out, a.lse, all, p.splits);
     else if (dim == 128)
