@@ -17,8 +17,10 @@
 //
 // Group scales: the sums are kept in units of the current group's scale and
 // multiplied by the ratio of the old scale to the new one where a group ends
-// (one fp32 product, where a second set of accumulators would not fit); scales
-// of zero, whose ratio is not finite, keep the unit and clear the group's codes.
+// (one fp32 product, where a second set of accumulators would not fit).  A
+// group whose scale is zero, or 2^-60 of the row's largest before it, keeps the
+// unit and has its codes cleared: in units of its scale the sums would pass
+// fp32, and it adds less than fp32 resolves of what such scales stand for.
 #pragma once
 
 #include "lm_matmul.h"
@@ -292,11 +294,11 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 acc[m][n][i] = 0.f;
-    float unit[WF];
-    uint32_t clear[WF];  // 0 where the group's codes count
+    float unit[WF], top[WF];  // the sums' unit, the largest scale so far
+    uint32_t clear[WF];       // 0 where the group's codes count
 #pragma unroll
     for (int n = 0; n < WF; ++n)
-        unit[n] = 1.f, clear[n] = 0;
+        unit[n] = 1.f, top[n] = 0.f, clear[n] = 0;
 
     const int32_t steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
     constexpr int BLOCKS = S::KS / 32;
@@ -352,11 +354,11 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 const int at = !GATED ? (wave * WF + n) * 32 + l32
                                : WF == 2 ? n * 128 + wave * 32 + l32 : (l32 >> 4) * 64 + wave * 16 + (l32 & 15);
                 const float sc = ss[at * 4 + (group & 3) + max(0, 4 * quad - sleft[n])];
-                const float ratio = k == begin * S::KS ? 0.f : unit[n] / sc;
-                const bool zero = sc == 0.f || __builtin_isinf(ratio);
-                clear[n] = zero ? 0xFFFFFFFFu : 0;
-                f[b][n] = zero || k == begin * S::KS ? 1.f : ratio;
-                unit[n] = zero ? unit[n] : sc;
+                const bool small = __builtin_fabsf(sc) * 0x1p60f < top[n] || sc == 0.f;
+                clear[n] = small ? 0xFFFFFFFFu : 0;
+                f[b][n] = small || top[n] == 0.f ? 1.f : unit[n] / sc;  // (no sums yet)
+                unit[n] = small ? unit[n] : sc;
+                top[n] = fmaxf(top[n], __builtin_fabsf(sc));
             }
             return true;
         }

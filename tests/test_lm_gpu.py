@@ -595,3 +595,22 @@ def test_matmul_zero_and_uneven_scales(lm, bits, r):
         s[6, 1] = -s[6, 1]
         s[7, 0] = 1e-42  # no normal number
         check_matmul(lm, L, bits)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2, 1])
+@pytest.mark.parametrize("r", [3, 20, 70, 300])
+def test_matmul_scales_of_empty_groups(lm, bits, r):
+    """Groups that a quantizer gave the smallest scale there is, beside ordinary ones: nothing passes fp32."""
+    g = gen(bits + r)
+    for group in (32, 64, 128):
+        for tiny in (torch.finfo(torch.float32).tiny, 1e-45, 1e-30):
+            L = layer(g, r, 1280, 150, bits, group, BF)
+            L["x"] *= 1000
+            s = L["scale"]
+            empty = torch.rand(s.shape, generator=g, device="cuda") < 0.4
+            empty[:, 2], empty[3, -1], empty[4, 0] = False, False, False  # (the results are normal numbers)
+            s[empty] = tiny
+            s[3, :-1], s[4, 1:] = tiny, tiny
+            s[6, 0], s[6, 1] = 0, tiny
+            s[7] = 10.0 ** -torch.arange(s.shape[1], device="cuda")  # down by tens
+            check_matmul(lm, L, bits)
