@@ -1,4 +1,7 @@
 // The linear layer: instances by type and width of weights.
+#include <algorithm>
+#include <cmath>
+
 #include "lm_internal.h"
 
 namespace qnn_lm {
@@ -38,12 +41,22 @@ static hipError_t launch_f16(const MatmulArgs &a, int bits, void *ws, hipStream_
     return hipErrorInvalidValue;
 }
 
-// Measured rules (see the kernels' heads):
-//   up to 16 rows the weights go straight to registers; above, x is worth
+// Rules, with what was measured on both sides (us; bf16, 4-bit weights in groups
+// of 128 unless said; x rows by columns to outputs):
+//   Up to 16 rows the weights go straight to registers; above, x is worth
 //   sharing through local memory.
-//   Tiles of 128 x 256 where they fill the 256 compute units twice over; else
-//   tiles of 64 rows of x, and of 128 rows of weights, and pieces of k, until
-//   there are workgroups enough.
+//   Tiles of 128 x 256 where they fill the 256 compute units twice over (4096 x
+//   11264 to 4096), else tiles of 64 rows of x (1024 x 4096 to 8192, 8 bits: 79
+//   against 90), and of 128 rows of weights where those of 256 do not fill them
+//   either (256 x 4096 to 14336: 51 against 64); 32 rows of x where there are
+//   no more (32 x 4096 to 22528: 25 against 28).
+//   Pieces of k shorten a workgroup's chain of steps, which bounds small grids,
+//   and cost their sums' way through memory: about the square root of the chain
+//   over the sums, and one more where that asks no compute unit for another
+//   workgroup.  128 x 4096 to 4096: 20 in 4 pieces, 25 in 2, 22.5 in 8; 16-bit
+//   weights, 256 x 4096 to 4096: 23 in 2, 29.5 whole, 26 in 4; 128 x 4096 to
+//   14336: 31 whole, 37 in 2; gated, 64 x 4096 to 11264: 33 in 4, 42 whole, 37
+//   in 2.
 TilePlan plan_matmul(const MatmulArgs &a, int bits)
 {
     TilePlan p = {0, 0, 1, (a.k + 127) / 128 * 128};
@@ -68,13 +81,13 @@ TilePlan plan_matmul(const MatmulArgs &a, int bits)
         return p;
     const int64_t groups = count(p.tf, p.wf);
     const int32_t blocks = (a.k + 127) / 128;
-    int32_t splits = (int32_t)(512 / groups);
-    if (splits > blocks / 4)
-        splits = blocks / 4;
-    if (splits > 8)
-        splits = 8;
+    const float chain = bits == 16 ? 1000.f : bits == 8 ? 1900.f : 2500.f;
+    int64_t splits = (int64_t)(sqrtf(chain * (float)a.k / ((float)a.r * (float)rows)) + 0.5f);
+    if (splits > 0 && (groups * (splits + 1) + 255) / 256 == (groups * splits + 255) / 256)
+        ++splits;
+    splits = std::min({splits, 768 / groups, (int64_t)blocks / 4, (int64_t)8});
     if (splits > 1) {
-        p.columns = (blocks + splits - 1) / splits * 128;
+        p.columns = (int32_t)((blocks + splits - 1) / splits * 128);
         p.splits = (a.k + p.columns - 1) / p.columns;
     }
     return p;

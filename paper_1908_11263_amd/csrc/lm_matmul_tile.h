@@ -620,10 +620,23 @@ __global__ void __launch_bounds__(256) matmul_join_kernel(MatmulArgs a, int32_t 
     const float *p = part + row * rows + col;
     f4 t = {0, 0, 0, 0}, up = {0, 0, 0, 0};
     if (a.m % 4 == 0) {
-        for (int s = 0; s < splits; ++s) {
-            t += *(const f4 *)(p + s * all);
-            if (a.gated)
-                up += *(const f4 *)(p + s * all + a.m);
+        // (four pieces' loads at a time; past the last piece it is read again)
+        for (int s = 0; s < splits; s += 4) {
+            f4 v[4], w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float *q = p + min(s + i, splits - 1) * all;
+                v[i] = *(const f4 *)q;
+                if (a.gated)
+                    w[i] = *(const f4 *)(q + a.m);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s + i < splits) {
+                    t += v[i];
+                    if (a.gated)
+                        up += w[i];
+                }
         }
     } else {
         for (int s = 0; s < splits; ++s)
