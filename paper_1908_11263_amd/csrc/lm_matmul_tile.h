@@ -256,12 +256,10 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
-    // Part PART of PARTS of a step's copies.
-    auto issue = [&](auto part, auto parts, int32_t step, int buf) {
-        constexpr int PART = part(), PARTS = parts();
+    auto issue = [&](int32_t step, int buf) {
         const int32_t k0 = step * S::KS, left = a.k - k0;  // a multiple of 32
         const uint32_t at = lds0 + buf * S::kStage;
-        if constexpr (GPB && PART == 0) {
+        if constexpr (GPB) {
             // before the step's other copies: those are counted, this one is not
             const int32_t quad = k0 >> gshift >> 2;
             if (step == begin || (k0 & ((4 << gshift) - 1)) == 0) {
@@ -275,29 +273,24 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         const int64_t w = (int64_t)k0 * BITS / 8;
         const uint32_t xat = at + wave * S::kXCopies * 1024,
                        wat = at + S::kXBytes + wave * S::kWCopies * 64 * S::kWUnit;
-        // (past the row's end, in pieces never read, its first ones are copied again)
-        const bool all = left >= S::KS;
+        if (left >= S::KS) {
 #pragma unroll
-        for (int i = 0; i < S::kXCopies; ++i)
-            if (i % PARTS == PART) {
-                if (all)
-                    copy_to_lds<16>(x, xo[i], xat + i * 1024);
-                else
-                    copy_to_lds<16>(x, xc[i] * 8 < left ? xo[i] : xo[i] - xc[i] * 16, xat + i * 1024);
-            }
+            for (int i = 0; i < S::kXCopies; ++i)
+                copy_to_lds<16>(x, xo[i], xat + i * 1024);
 #pragma unroll
-        for (int i = 0; i < S::kWCopies; ++i)
-            if ((S::kXCopies + i) % PARTS == PART) {
-                if (all)
-                    copy_to_lds<S::kWUnit>(wb[i] + w, wo[i], wat + i * 64 * S::kWUnit);
-                else
-                    copy_to_lds<S::kWUnit>(wb[i] + w, wc[i] * (S::kWUnit * 8 / BITS) < left ? wo[i] : wo[i] - wc[i] * S::kWUnit,
-                                           wat + i * 64 * S::kWUnit);
-            }
+            for (int i = 0; i < S::kWCopies; ++i)
+                copy_to_lds<S::kWUnit>(wb[i] + w, wo[i], wat + i * 64 * S::kWUnit);
+        } else {
+            // pieces past the row's end, never read, copy its first again
+#pragma unroll
+            for (int i = 0; i < S::kXCopies; ++i)
+                copy_to_lds<16>(x, xc[i] * 8 < left ? xo[i] : xo[i] - xc[i] * 16, xat + i * 1024);
+#pragma unroll
+            for (int i = 0; i < S::kWCopies; ++i)
+                copy_to_lds<S::kWUnit>(wb[i] + w, wc[i] * (S::kWUnit * 8 / BITS) < left ? wo[i] : wo[i] - wc[i] * S::kWUnit,
+                                       wat + i * 64 * S::kWUnit);
+        }
     };
-    constexpr std::integral_constant<int, 0> P0;
-    constexpr std::integral_constant<int, 1> P1;
-    constexpr std::integral_constant<int, 2> P2;
 
     f16v acc[TF][WF];
 #pragma unroll
@@ -392,12 +385,10 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
 
 #pragma unroll
     for (int s = 0; s < S::kStages - 1; ++s)
-        issue(P0, P1, min(begin + s, steps - 1), s);
+        issue(min(begin + s, steps - 1), s);
     wait_copies<(S::kStages - 2) * S::kCopies>();
     __builtin_amdgcn_s_barrier();
-    // A step's copies go to the place of the step before, which has been read,
-    // in parts between the products (past the last step they are the last
-    // one's, so that the counts stay).
+    issue(min(begin + S::kStages - 1, steps - 1), S::kStages - 1);
     int buf = 0;
     // (k is a multiple of 32: the last step of all may be one block)
     const bool half_step = BLOCKS == 2 && steps * S::KS > a.k;
@@ -410,30 +401,26 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
         fetch<N, BITS, TF, WF, GPB, 0>(lds, raw[0], clear, 0, l32, half, pair[0]);
         for (int32_t s = begin; s < whole; ++s) {
             const uint8_t *xs = lds + buf * S::kStage;
-            const int fill = buf == 0 ? S::kStages - 1 : buf - 1;
-            const int32_t later = min(s + S::kStages - 1, steps - 1);
-            constexpr std::integral_constant<int, BLOCKS == 2 ? 3 : 2> PARTS;
-            issue(P0, PARTS, later, fill);
             if (GPB && scale)
                 rescale(0);
             fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[0], clear, 0, l32, half, pair[1]);
             multiply(pair[0]);
-            issue(P1, PARTS, later, fill);
             if constexpr (BLOCKS == 2) {
                 if constexpr (GPB == 2)
                     begins(s, 1);
                 fetch<N, BITS, TF, WF, GPB, 0>(xs, raw[1], clear, 1, l32, half, pair[0]);
                 multiply(pair[1]);
-                issue(P2, PARTS, later, fill);
                 if constexpr (GPB == 2)
                     rescale(1);
                 fetch<N, BITS, TF, WF, GPB, 1>(xs, raw[1], clear, 1, l32, half, pair[1]);
                 multiply(pair[0]);
             }
-            // everything of this step has been read; the next one's copies are
-            // waited for
+            // Everything of this step has been read: the next one's copies are
+            // waited for, and this one's place is filled again (past the last step
+            // with the last one, so that the counts stay).
             wait_copies<(S::kStages - 2) * S::kCopies>();
             __builtin_amdgcn_s_barrier();
+            issue(min(s + S::kStages, steps - 1), buf);
             buf = buf == S::kStages - 1 ? 0 : buf + 1;
             const uint8_t *xn = lds + buf * S::kStage;
             read_raw(xn + S::kXBytes);
@@ -489,10 +476,11 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                         bool &next_first) {
             if constexpr (GPB)
                 set_aside();
-            const int fill = buf == 0 ? S::kStages - 1 : buf - 1;
-            issue(P0, P1, min(s + S::kStages - 1, steps - 1), fill);
+            // Step s has been read: its place is filled again (past the last
+            // step with the last one, so that the counts stay).
             wait_copies<(S::kStages - 2) * S::kCopies>();
             __builtin_amdgcn_s_barrier();
+            issue(min(s + S::kStages, steps - 1), buf);
             buf = buf == S::kStages - 1 ? 0 : buf + 1;
             prepare(s + 1, next, next_first);
             if (GPB && first)
