@@ -14,25 +14,86 @@ struct TokenArgs {
     const void *k, *v;
     int64_t ks[3], vs[3];  // elements: sequence, token, head
     int32_t t;
-    uint32_t tokens;       // b * t * 2 * heads
+    uint32_t tokens;       // b * t * heads
     qnn::FastDiv heads_div, t_div;
     const int32_t *lens, *counts;
 };
 
-// Index of this thread's token: (sequence, token, key or value, head), the
-// head fastest.
+// Index of this thread's token: (sequence, token, head), the head fastest.  A
+// thread does its key and its value: they have the place in common.
 struct Token {
-    int32_t seq, i, which, head;
+    int32_t seq, i, head;
 };
 __device__ __forceinline__ Token token_of(uint32_t n, const qnn::FastDiv &heads, const qnn::FastDiv &t)
 {
     Token o;
-    const uint32_t a = qnn::fdiv(n, heads), b = a >> 1;
+    const uint32_t a = qnn::fdiv(n, heads);
     o.head = n - a * heads.d;
-    o.which = a & 1;
-    o.seq = qnn::fdiv(b, t);
-    o.i = b - o.seq * t.d;
+    o.seq = qnn::fdiv(a, t);
+    o.i = a - o.seq * t.d;
     return o;
+}
+
+// Codes of a token's eight numbers w (its LANES lanes hold them all), and its
+// scale: the largest magnitude over the largest code.
+template <class N, int BITS, int LANES>
+__device__ __forceinline__ u2 codes_of(u4 w, float &scale)
+{
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    constexpr bool BF = __is_same(N, Bf16);
+    constexpr float most = BITS == 8 ? 127.f : 7.f;
+    // the largest magnitude, by bits: infinity and NaN are above every finite number
+    us2 m = __builtin_bit_cast(us2, w[0] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, w[i] & 0x7FFF7FFFu));
+    uint32_t top = max(m[0], m[1]);
+#pragma unroll
+    for (int i = 1; i < LANES; i <<= 1)
+        top = max(top, (uint32_t)__shfl_xor((int)top, i, 64));
+    auto number = [](uint32_t bits) {
+        return BF ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+    };
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = number(w[i] & 0xFFFFu);
+        v[2 * i + 1] = BF ? __uint_as_float(w[i] & 0xFFFF0000u) : number(w[i] >> 16);
+    }
+    const bool finite = top < (BF ? 0x7F80u : 0x7C00u);
+    scale = finite ? number(top) / most : __uint_as_float(0x7FC00000u);
+    // v / scale, correctly rounded: with the correctly rounded reciprocal y, q =
+    // v y is within a unit, and q + (v - q scale) y rounds as the quotient does
+    // (Markstein).  It is above the largest code by its own rounding at most;
+    // adding 1.5 2^23 rounds it to a whole number, whose low bits are the code.
+    uint32_t code[8];
+    if (__any(!finite || (scale > 0.f && scale < 0x1p-100f))) {
+        // scales whose reciprocal is not a normal number divide
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            code[e] = (uint32_t)(int32_t)fminf(fmaxf(rintf(finite && scale > 0.f ? v[e] / scale : 0.f), -most), most);
+    } else {
+        const float y = scale > 0.f ? 1.f / scale : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q = v[e] * y;
+            code[e] = __float_as_uint(__builtin_fmaf(__builtin_fmaf(-q, scale, v[e]), y, q) + 0x1.8p23f);
+        }
+    }
+    u2 r = {0, 0};
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            r[i] = __builtin_amdgcn_perm(code[4 * i + 1], code[4 * i], 0x0C0C0400u) |
+                   __builtin_amdgcn_perm(code[4 * i + 3], code[4 * i + 2], 0x04000C0Cu);
+    } else {
+        uint32_t pair[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            pair[i] = (code[2 * i] & 15u) | code[2 * i + 1] << 4;
+        r[0] = __builtin_amdgcn_perm(pair[1], pair[0], 0x0C0C0400u) | __builtin_amdgcn_perm(pair[3], pair[2], 0x04000C0Cu);
+    }
+    return r;
 }
 
 template <class N, int BITS, int DIM>
@@ -49,69 +110,35 @@ __global__ void __launch_bounds__(256) append_kernel(CacheArgs c, TokenArgs a)
     const Slot s = find_slot(c, o.seq, (int64_t)a.lens[o.seq] + o.i);
     if (s.page < 0)
         return;
-    const int64_t *st = o.which ? a.vs : a.ks;
-    const typename N::T *src =
-        (const typename N::T *)(o.which ? a.v : a.k) + o.seq * st[0] + o.i * st[1] + o.head * st[2] + lane * 8;
-    uint8_t *dst = o.which ? c.v + s.page * c.v_page + o.head * c.v_head + s.slot * c.v_slot
-                           : c.k + s.page * c.k_page + o.head * c.k_head + s.slot * c.k_slot;
+    const u4 kw = *(const u4 *)((const typename N::T *)a.k + o.seq * a.ks[0] + o.i * a.ks[1] + o.head * a.ks[2] + lane * 8);
+    const u4 vw = *(const u4 *)((const typename N::T *)a.v + o.seq * a.vs[0] + o.i * a.vs[1] + o.head * a.vs[2] + lane * 8);
+    uint8_t *kd = c.k + s.page * c.k_page + o.head * c.k_head + s.slot * c.k_slot + lane * BITS;
+    uint8_t *vd = c.v + s.page * c.v_page + o.head * c.v_head + s.slot * c.v_slot + lane * BITS;
     if constexpr (BITS == 16) {
-        *(u4 *)(dst + lane * 16) = *(const u4 *)src;
+        *(u4 *)kd = kw;
+        *(u4 *)vd = vw;
     } else {
-        float v[8];
-        load8<N>(src, 0, v);
-        // the largest magnitude, by bits: infinity and NaN are above every finite number
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-#pragma unroll
-        for (int m = 1; m < LANES; m <<= 1)
-            top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
-        constexpr float most = BITS == 8 ? 127.f : 7.f;
-        const bool finite = top < 0x7F800000u;
-        const float scale = finite ? __uint_as_float(top) / most : __uint_as_float(0x7FC00000u);
-        // v / scale, correctly rounded: with the correctly rounded reciprocal y,
-        // q = v y is within a unit, and q + (v - q scale) y rounds as the quotient
-        // does (Markstein), three operations for each of a token's numbers.
-        // Scales whose reciprocal is not a normal number divide.
-        uint32_t code[8];
-        const bool normal = scale >= 0x1p-100f;
-        const float y = normal ? 1.f / scale : 0.f;
-        if (__any(finite && scale > 0.f && !normal)) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = finite && scale > 0.f ? v[e] / scale : 0.f;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float q = v[e] * y;
-                v[e] = finite ? __builtin_fmaf(__builtin_fmaf(-q, scale, v[e]), y, q) : 0.f;
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            code[e] = (uint32_t)(int32_t)fminf(fmaxf(rintf(v[e]), -most), most);
+        float ks, vs;
+        const u2 kc = codes_of<N, BITS, LANES>(kw, ks), vc = codes_of<N, BITS, LANES>(vw, vs);
         if constexpr (BITS == 8) {
-            u2 r;
-            r.x = (code[0] & 255) | (code[1] & 255) << 8 | (code[2] & 255) << 16 | code[3] << 24;
-            r.y = (code[4] & 255) | (code[5] & 255) << 8 | (code[6] & 255) << 16 | code[7] << 24;
-            *(u2 *)(dst + lane * 8) = r;
+            *(u2 *)kd = kc;
+            *(u2 *)vd = vc;
         } else {
-            uint32_t r = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                r |= (code[e] & 15) << 4 * e;
-            *(uint32_t *)(dst + lane * 4) = r;
+            *(uint32_t *)kd = kc[0];
+            *(uint32_t *)vd = vc[0];
         }
-        if (lane == 0)
-            (o.which ? c.v_scale : c.k_scale)[scale_at(c, s, o.head)] = scale;
+        if (lane == 0) {
+            const int64_t at = scale_at(c, s, o.head);
+            c.k_scale[at] = ks;
+            c.v_scale[at] = vs;
+        }
     }
 }
 
 struct ReadArgs {
     void *k, *v;
     int32_t t;
-    uint32_t tokens;          // b * t * 2 * heads
+    uint32_t tokens;          // b * t * heads
     qnn::FastDiv heads_div, t_div;
     const int32_t *start;
 };
@@ -126,33 +153,34 @@ __global__ void __launch_bounds__(256) read_kernel(CacheArgs c, ReadArgs a)
     if (n >= a.tokens)
         return;
     const Token o = token_of(n, a.heads_div, a.t_div);
-    void *dst = o.which ? a.v : a.k;
-    if (!dst)
-        return;
     const int64_t at = (((int64_t)o.seq * a.t + o.i) * c.heads + o.head) * DIM + lane * 8;
     const Slot s = find_slot(c, o.seq, (int64_t)a.start[o.seq] + o.i);
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (s.page >= 0) {
-        const uint8_t *src = o.which ? c.v + s.page * c.v_page + o.head * c.v_head + s.slot * c.v_slot
-                                     : c.k + s.page * c.k_page + o.head * c.k_head + s.slot * c.k_slot;
-        if constexpr (BITS == 16) {
-            load8<C>(src, lane * 8, v);
-        } else {
-            const float scale = (o.which ? c.v_scale : c.k_scale)[scale_at(c, s, o.head)];
-            if constexpr (BITS == 8) {
-                const u2 r = *(const u2 *)(src + lane * 8);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] = (float)(int8_t)(r[e / 4] >> 8 * (e % 4)) * scale;
+    auto one = [&](void *dst, const uint8_t *src, const float *scales) {
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (s.page >= 0) {
+            if constexpr (BITS == 16) {
+                load8<C>(src, 0, v);
             } else {
-                const uint32_t r = *(const uint32_t *)(src + lane * 4);
+                const float scale = scales[scale_at(c, s, o.head)];
+                if constexpr (BITS == 8) {
+                    const u2 r = *(const u2 *)src;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] = (float)((int32_t)(r << (28 - 4 * e)) >> 28) * scale;
+                    for (int e = 0; e < 8; ++e)
+                        v[e] = (float)(int8_t)(r[e / 4] >> 8 * (e % 4)) * scale;
+                } else {
+                    const uint32_t r = *(const uint32_t *)src;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[e] = (float)((int32_t)(r << (28 - 4 * e)) >> 28) * scale;
+                }
             }
         }
-    }
-    store8<N>(dst, at, v);
+        store8<N>(dst, at, v);
+    };
+    if (a.k)
+        one(a.k, c.k + s.page * c.k_page + o.head * c.k_head + s.slot * c.k_slot + lane * BITS, c.k_scale);
+    if (a.v)
+        one(a.v, c.v + s.page * c.v_page + o.head * c.v_head + s.slot * c.v_slot + lane * BITS, c.v_scale);
 }
 
 // A workgroup owns the keys or the values of one head of one sequence, and
@@ -230,7 +258,7 @@ hipError_t launch_append(const CacheArgs &c, int bits, int dim, int type, const 
         a.vs[i] = v_stride[i];
     }
     a.t = t;
-    a.tokens = (uint32_t)((int64_t)c.b * t * 2 * c.heads);
+    a.tokens = (uint32_t)((int64_t)c.b * t * c.heads);
     a.heads_div = qnn::make_fastdiv((uint32_t)c.heads);
     a.t_div = qnn::make_fastdiv((uint32_t)t);
     a.lens = lens;
@@ -269,7 +297,7 @@ hipError_t launch_read(const CacheArgs &c, int bits, int dim, int type, int cach
     a.k = k;
     a.v = v;
     a.t = t;
-    a.tokens = (uint32_t)((int64_t)c.b * t * 2 * c.heads);
+    a.tokens = (uint32_t)((int64_t)c.b * t * c.heads);
     a.heads_div = qnn::make_fastdiv((uint32_t)c.heads);
     a.t_div = qnn::make_fastdiv((uint32_t)t);
     a.start = start;
