@@ -2,10 +2,12 @@
 // cache_read.  All are bound by memory (and, for a few tokens, by the launch):
 // DIM / 8 lanes own a token of a head, eight channels each, so that every
 // access is 16 bytes of numbers or the 4 to 16 bytes of their codes.
-//   Append of 4 x 4001 tokens of 8 heads of 128 at 4 bits: 31 us (the division
-//   of each number by its token's scale, exact to the last bit, bounds it: 2.7
-//   TB/s); reading them back 21 us, 4 TB/s.  A few tokens: 3.4 us, and 2.9
-//   for the read; keep of 64 sequences' trees of 33: 3.8 us.
+// A thread does a token's key and its value, as working their place out takes
+// as many instructions as a row's codes do (one of the two a thread: 30 us where
+// it takes 20 now).
+//   Append of 4 x 4001 tokens of 8 heads of 128 at 4 bits: 20 us (4.2 TB/s);
+//   reading them back 17.5 us (4.7 TB/s).  8 x 16 tokens at 8 bits: 4.2 us, and 3
+//   for the read; keep of 64 sequences' trees of 33: 3.9 us.
 #include "lm_cache.h"
 
 namespace qnn_lm {
