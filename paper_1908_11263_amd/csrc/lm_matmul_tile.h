@@ -14,7 +14,7 @@
 // address that a lane reads from memory.
 //   4096 x 4096 to 8192, bf16: 4 bits and a scale a row 252 us (1089 TFLOP/s),
 //   in groups of 128 284 us, 8 bits 264 us, 16 bits 291 us, 2 bits in groups 302
-//   us; 4096 x 11264 to 4096, 4 bits in groups: 380 us (995 TFLOP/s).  A product
+//   us; 4096 x 11264 to 4096, 4 bits in groups: 375 us (1007 TFLOP/s).  A product
 //   of two 16-bit matrices of the first size takes 1510 to 1600 TFLOP/s in a
 //   library.
 //
