@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
     auto step = [&](Ahead &h, int32_t t) {
         uint8_t *buf = lds + ((t - first) & 1) * S::kBuffer;
         const uint64_t there = h.valid;
-        if (BITS != 16 && there != S::kWhole && !((there >> lane) & 1))
+        // (a lane past a tile of 32 has no position: what it has read is another's)
+        if (BITS != 16 && (KT < 64 || there != S::kWhole) && !((there >> lane) & 1))
             h.ks = h.vs = 0.f;
         const float vsmine = BITS == 16 ? 0.f : h.vs;
         if constexpr (BITS != 16) {

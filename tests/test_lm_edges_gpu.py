@@ -1,0 +1,46 @@
+"""The operators of include/qnn_lm.h where numbers are not ordinary: NaN and
+infinities, scales far apart or negative, places that a call must not look at.
+Against the formulas in 64 bits (lm_reference.py), with its bounds."""
+import math
+
+import pytest
+import torch
+
+import lm_reference as ref
+from test_lm_gpu import lm, gen, randn, make_cache, words, layer  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, F = torch.bfloat16, torch.float16, torch.float32
+ROWS = [(1, 4), (5, 4), (20, 2), (40, 2)]  # drafts and query heads of a cache head: few rows to many
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def check(lm, q, cache, table, lens, mask=None, extra=0.0):
+    t = q.shape[1]
+    out, lse = lm.tree_attention(q, cache, table, i32(lens), mask=None if mask is None else words(mask, t), want_lse=True)
+    wo, wl, eo, el = ref.attention(q, cache, table, lens, mask, None, q.shape[-1] ** -0.5)
+    ref.close(lse, wl, el, "lse")
+    ref.close(out, wo, eo + extra, "out")
+    return out, lse
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("t,g", [(5, 4), (20, 1), (9, 8)])
+def test_scales_of_other_sequences(lm, bits, t, g):
+    """A scale that belongs to no position of the sequence (the cache's very first place, on a page that the table does
+    not name) changes no bit, whatever it holds."""
+    for dim in (256, 128, 64):
+        r = gen(dim + t)
+        cache = make_cache(lm, r, 8, 1, 32, dim, bits, BF)
+        table = i32([[3, 5, 1, 7]])
+        q = randn(r, 1, t, g, dim, dtype=BF)
+        base = lm.tree_attention(q, cache, table, i32([96 - t]), want_lse=True)
+        for huge in (1e6, 1e12, 1e30, math.inf, math.nan):
+            vs, ks = cache.v_scale.clone(), cache.k_scale.clone()
+            vs[0, 0, 0] = ks[0, 0, 0] = huge
+            got = lm.tree_attention(q, cache._replace(v_scale=vs, k_scale=ks), table, i32([96 - t]), want_lse=True)
+            assert torch.equal(got[0], base[0]) and torch.equal(got[1], base[1]), (dim, huge)
