@@ -85,6 +85,16 @@ __device__ __forceinline__ uint64_t seen_bits(const AttendArgs &a, int32_t seq, 
     return s ? lo >> s | hi << (64 - s) : lo;
 }
 
+// Whether a row (draft < 0: one of no draft) has seen nothing; m is then
+// -infinity.  NaN scores raise no maximum: a row that has seen nothing else gets
+// the maximum 0, so that its sum, NaN, is not taken for nothing.
+__device__ __forceinline__ bool seen_nothing(int32_t draft, float &m, float l)
+{
+    const bool none = draft < 0 || (m == -INFINITY && l == 0.f);
+    m = none ? -INFINITY : m == -INFINITY ? 0.f : m;
+    return none;
+}
+
 // A row's result from its sum l, maximum m (in powers of two) and outputs
 // v = 4 channels at d: into the pieces, or finished.
 template <class N, int DIM>

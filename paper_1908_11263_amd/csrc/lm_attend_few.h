@@ -395,8 +395,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
     for (int n = 0; n < NR; ++n) {
         l[n] += __shfl_xor(l[n], 16, 64);
         l[n] += __shfl_xor(l[n], 32, 64);
-        if (draft[n] < 0)
-            m[n] = -INFINITY;  // no draft of this sequence: has seen nothing
+        const bool none = seen_nothing(draft[n], m[n], l[n]);
         __syncthreads();
         if (kq == 0) {
             jm[wave * 16 + l16] = m[n];
@@ -413,7 +412,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
 #pragma unroll
         for (int d = 0; d < ND; ++d)
             // (a row that has seen nothing may hold anything)
-            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = m[n] == -INFINITY ? (f4){0, 0, 0, 0} : o[n][d] * f;
+            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = none ? (f4){0, 0, 0, 0} : o[n][d] * f;
         __syncthreads();
         // 16 threads a row
         const int r = threadIdx.x >> 4, e0 = threadIdx.x & 15;

@@ -398,9 +398,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
         const int32_t row = row0 + n * 16 + l16;
         if (row >= pl.rows)
             continue;
-        if (draft[n] < 0)
-            m[n] = -INFINITY;  // no draft of this sequence: has seen nothing
-        const bool none = m[n] == -INFINITY;
+        const bool none = seen_nothing(draft[n], m[n], l[n]);
         const int32_t dr = row / pl.g;
         const int64_t index = ((int64_t)seq * a.t + dr) * a.heads + head * pl.g + row - dr * pl.g;
         const float inv = none ? 0.f : 1.f / l[n];

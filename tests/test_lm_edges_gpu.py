@@ -44,3 +44,53 @@ def test_scales_of_other_sequences(lm, bits, t, g):
             vs[0, 0, 0] = ks[0, 0, 0] = huge
             got = lm.tree_attention(q, cache._replace(v_scale=vs, k_scale=ks), table, i32([96 - t]), want_lse=True)
             assert torch.equal(got[0], base[0]) and torch.equal(got[1], base[1]), (dim, huge)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("t,g", ROWS)
+@pytest.mark.parametrize("n", [20, 3000])
+def test_nan_queries(lm, bits, t, g, n):
+    """A query that holds NaN gives NaN, the rows beside it what they always give."""
+    r = gen(t + g + n)
+    page = 64
+    width = -(-(n + t) // page)
+    for dim, dtype in ((64, BF), (128, HF), (256, BF)):
+        cache = make_cache(lm, r, width, 1, page, dim, bits, dtype)
+        q = randn(r, 1, t, g, dim, dtype=dtype)
+        q[0, 0, 0, 5] = math.nan
+        q[0, t - 1, g - 1, dim - 1] = math.nan
+        out, lse = check(lm, q, cache, torch.arange(width, device="cuda", dtype=torch.int32).reshape(1, width), [n])
+        assert bool(out[0, 0, 0].isnan().all()) and bool(lse[0, 0, 0].isnan())
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("t,g", ROWS)
+def test_nan_keys(lm, bits, t, g):
+    """Keys that are NaN: all that a draft sees, or a stretch of a long cache that one wave or one piece has to itself."""
+    for dim, dtype in ((128, BF), (64, HF)):
+        r = gen(t + g + dim)
+        page = 32
+        width = -(-(3000 + t) // page)
+        table = torch.randperm(width, generator=r, device="cuda").int().reshape(1, width)
+        q = randn(r, 1, t, g, dim, dtype=dtype)
+
+        def spoiled(cache, positions):
+            k, ks = cache.k.clone(), None if bits == 16 else cache.k_scale.clone()
+            for pos in positions:
+                pg, slot = int(table[0, pos // page]), pos % page
+                if bits == 16:
+                    k[pg, :, slot] = math.nan
+                else:
+                    ks[pg, :, slot] = math.nan
+            return cache._replace(k=k, k_scale=ks)
+
+        cache = make_cache(lm, r, width, 1, page, dim, bits, dtype)
+        # an empty cache: draft 0 sees its own key alone
+        out, _ = check(lm, q, spoiled(cache, [0]), table, [0])
+        assert bool(out.isnan().all())
+        mask = [[[0] if i == 0 else [i] for i in range(t)]]
+        out, _ = check(lm, q, spoiled(cache, [0]), table, [0], mask)
+        assert bool(out[0, 0].isnan().all()) and not bool(out[0, 1:].isnan().any())
+        for first, last in ((0, 32), (96, 128), (128, 256), (2944, 3000)):
+            out, _ = check(lm, q, spoiled(cache, range(first, last)), table, [3000])
+            assert bool(out.isnan().all()), first
