@@ -39,6 +39,9 @@ typedef __attribute__((address_space(3))) s4_ lds_s4;
 typedef __attribute__((address_space(3))) i2_ lds_i2;
 
 constexpr float kAbove = 10.f, kSlack = 4.f;
+// Factor that a piece of the positions joins the others with, at least: finite
+// outputs do not change by it, an infinite one stays so.
+constexpr float kLeast = 0x1p-126f;
 
 struct AttendPlan {
     int32_t g;          // query heads of a cache head
@@ -152,6 +155,80 @@ __device__ __forceinline__ f4 add_odd_values(s8_ v, typename P::V8 p, typename P
         o[i] += c[i] > 0.f ? NAN : 0.f;
     }
     return o;
+}
+
+// Whether a row that has seen numbers only has an output that is NaN.
+template <int NR, int ND>
+__device__ __forceinline__ bool any_nan(const f4 (&o)[NR][ND], const float (&l)[NR])
+{
+    bool nan = false;
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                nan |= o[n][d][i] != o[n][d][i] && l[n] == l[n];
+    return __any(nan);
+}
+
+// Outputs that are NaN though the values that their row has seen in the channel
+// are infinite of one sign at most: an infinity times a probability below the
+// smallest 16-bit number, or times a probability's negative second number.  They
+// become that infinity.  Whoever calls this has found a NaN; it reads the
+// values of the wave's tiles (first, first + stride .. of `tile` positions)
+// again, which looking for infinities in every tile would cost all calls.
+template <class N, int DIM, int NR>
+__device__ __forceinline__ void settle_infinities(const AttendArgs &a, const CacheArgs &c, int32_t seq, int32_t head,
+                                                  const int32_t (&draft)[NR], int32_t len, int32_t first, int32_t last,
+                                                  int32_t stride, int32_t tile, int32_t end, f4 (&o)[NR][DIM / 16])
+{
+    constexpr int ND = DIM / 16;
+    constexpr uint32_t inf = __is_same(N, Bf16) ? 0x7F80 : 0x7C00;
+    const int kq = (threadIdx.x & 63) >> 4;
+    uint64_t up[NR], down[NR], nan[NR];  // bit 4 d + i: of this lane's channel i of sixteen d
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+        up[n] = down[n] = nan[n] = 0;
+#pragma unroll 1
+    for (int32_t t = first; t < last; t += stride)
+#pragma unroll 1
+        for (int32_t pos = t * tile; pos < min((t + 1) * tile, end); ++pos) {
+            const Slot s = find_slot(c, seq, pos);
+            if (s.page < 0)
+                continue;
+            const uint8_t *p = c.v + s.page * c.v_page + head * c.v_head + s.slot * c.v_slot + kq * 8;
+            uint64_t u = 0, w = 0, x = 0;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const u2 r = *(const u2 *)(p + d * 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t v = r[i / 2] >> (16 * (i % 2)) & 0xFFFFu;
+                    const uint64_t bit = 1ull << (4 * d + i);
+                    u |= v == inf ? bit : 0;
+                    w |= v == (inf | 0x8000u) ? bit : 0;
+                    x |= (v & 0x7FFFu) > inf ? bit : 0;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+                if (draft[n] >= 0 && (seen_bits(a, seq, draft[n], pos, len) & 1)) {
+                    up[n] |= u;
+                    down[n] |= w;
+                    nan[n] |= x;
+                }
+        }
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t bit = 1ull << (4 * d + i);
+                if (o[n][d][i] != o[n][d][i] && ((up[n] ^ down[n]) & ~nan[n] & bit))
+                    o[n][d][i] = up[n] & bit ? INFINITY : -INFINITY;
+            }
 }
 
 // Largest exponent of the scales that lanes hold, at least -120 (zeros and what

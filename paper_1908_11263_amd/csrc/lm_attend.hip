@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float *part, void *out,
     for (int i = 0; i < 2; ++i) {
         const int s = i * 256 + tid;
         // (a piece that has seen nothing counts for nothing, whatever it holds)
-        const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
+        const float f = m[i] == -INFINITY ? 0.f : fmaxf(__builtin_amdgcn_exp2f(m[i] - top), kLeast);
         if (s < splits)
             factor[s] = f;
         sum += m[i] == -INFINITY ? 0.f : l[i] * f;

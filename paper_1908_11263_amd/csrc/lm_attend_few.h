@@ -388,13 +388,19 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         if (at + 4 < last)
             step(ahead[1], at + 4);
     }
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        l[n] += __shfl_xor(l[n], 16, 64);
+        l[n] += __shfl_xor(l[n], 32, 64);
+    }
+    if constexpr (BITS == 16)
+        if (any_nan<NR, ND>(o, l))
+            settle_infinities<N, DIM, NR>(a, c, seq, head, draft, sq.len, first, last, 4, kAttendTile, end, o);
     // join the four waves, sixteen rows at a time
     constexpr int OP = DIM + 4;  // pitch in floats
     float *jo = (float *)lds, *jm = jo + 4 * 16 * OP, *jl = jm + 64;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-        l[n] += __shfl_xor(l[n], 16, 64);
-        l[n] += __shfl_xor(l[n], 32, 64);
         const bool none = seen_nothing(draft[n], m[n], l[n]);
         __syncthreads();
         if (kq == 0) {
@@ -410,9 +416,15 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         if constexpr (BITS != 16)
             f = ldexpf(f, BITS == 4 ? vexp - 4 : vexp);
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
-            // (a row that has seen nothing may hold anything)
-            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = none ? (f4){0, 0, 0, 0} : o[n][d] * f;
+        for (int d = 0; d < ND; ++d) {
+            // (a row that has seen nothing may hold anything; an infinity stays
+            // one when the factor is zero)
+            f4 v = o[n][d] * f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = none ? 0.f : fabsf(o[n][d][i]) == INFINITY ? o[n][d][i] : v[i];
+            *(f4 *)(jo + (wave * 16 + l16) * OP + d * 16 + 4 * kq) = v;
+        }
         __syncthreads();
         // 16 threads a row
         const int r = threadIdx.x >> 4, e0 = threadIdx.x & 15;

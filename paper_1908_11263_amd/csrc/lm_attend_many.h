@@ -389,12 +389,18 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
             if (t + 1 < last)
                 step(ahead[1], t + 1);
     }
-    const int64_t all = (int64_t)c.b * a.t * a.heads;
-    const float f = BITS == 16 ? 1.f : ldexpf(1.f, BITS == 4 ? vexp - 4 : vexp);
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         l[n] += __shfl_xor(l[n], 16, 64);
         l[n] += __shfl_xor(l[n], 32, 64);
+    }
+    if constexpr (BITS == 16)
+        if (any_nan<NR, ND>(o, l))
+            settle_infinities<N, DIM, NR>(a, c, seq, head, draft, sq.len, first, last, 1, KT, end, o);
+    const int64_t all = (int64_t)c.b * a.t * a.heads;
+    const float f = BITS == 16 ? 1.f : ldexpf(1.f, BITS == 4 ? vexp - 4 : vexp);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
         const int32_t row = row0 + n * 16 + l16;
         if (row >= pl.rows)
             continue;

@@ -94,3 +94,48 @@ def test_nan_keys(lm, bits, t, g):
         for first, last in ((0, 32), (96, 128), (128, 256), (2944, 3000)):
             out, _ = check(lm, q, spoiled(cache, range(first, last)), table, [3000])
             assert bool(out.isnan().all()), first
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("t,g", ROWS)
+@pytest.mark.parametrize("low", [False, True])
+def test_infinite_values(lm, dtype, t, g, low):
+    """Infinite values of cached tokens, in tiles that every row sees whole: infinities of their sign, NaN where both
+    signs meet, the other channels as ever; also where such a token's probability is below the smallest 16-bit number."""
+    for dim in (64, 128, 256):
+        for n in (200, 2000):
+            r = gen(t + dim)
+            page = 16
+            width = -(-(n + t) // page)
+            table = torch.randperm(width, generator=r, device="cuda").int().reshape(1, width)
+            cache = make_cache(lm, r, width, 1, page, dim, 16, dtype)
+            base = randn(r, dim)
+            q = (base + 0.1 * randn(r, 1, t, g, dim)).to(dtype)
+            for pos, channel, what in ((70, 3, math.inf), (90, 5, -math.inf), (71, 7, math.inf), (140, 7, -math.inf),
+                                       (n - 1, 9, math.inf)):
+                pg, slot = int(table[0, pos // page]), pos % page
+                cache.v[pg, 0, slot, channel] = what
+                if low:
+                    # scores about 50 below the others'
+                    cache.k[pg, 0, slot] = (base * (-50 * dim ** 0.5 / float(base @ base))).to(dtype)
+            out, _ = check(lm, q, cache, table, [n])
+            assert bool(out[..., 3].isposinf().all()) and bool(out[..., 5].isneginf().all())
+            assert bool(out[..., 7].isnan().all()) and bool(out[..., 9].isposinf().all())
+
+
+@pytest.mark.parametrize("t,g", ROWS)
+def test_infinite_values_far_below(lm, t, g):
+    """An infinite value in a stretch of positions whose scores all lie 100 below the others': no factor between parts
+    of the positions makes zero of it."""
+    for dim in (64, 128, 256):
+        for n in (200, 2000):
+            r = gen(t + dim)
+            page = 32
+            width = -(-(n + t) // page)
+            cache = make_cache(lm, r, width, 1, page, dim, 16, BF)
+            base = randn(r, dim)
+            q = (base + 0.1 * randn(r, 1, t, g, dim)).to(BF)
+            cache.k[1:5, 0] = (base * (-100 * dim ** 0.5 / float(base @ base))).to(BF)
+            cache.v[2, 0, 9, 3] = math.inf
+            out, _ = check(lm, q, cache, torch.arange(width, device="cuda", dtype=torch.int32).reshape(1, width), [n])
+            assert bool(out[..., 3].isposinf().all())
