@@ -231,6 +231,14 @@ __device__ __forceinline__ void settle_infinities(const AttendArgs &a, const Cac
             }
 }
 
+// A probability's product with its value's scale, in a tile that holds a scale
+// that is not finite: nothing where the position is not seen, whatever it holds
+// there, and the infinity however small the probability.
+__device__ __forceinline__ float odd_product(float score, float scale, float product)
+{
+    return score == -INFINITY ? 0.f : fabsf(scale) == INFINITY ? scale : product;
+}
+
 // Largest exponent of the scales that lanes hold, at least -120 (zeros and what
 // is not finite do not count).
 template <int LANES>

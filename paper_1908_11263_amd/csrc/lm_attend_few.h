@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                 s[n][u] *= ks[u];
         }
         const bool whole = there == 0xFFFFFFFFu && p0 + kAttendTile <= sq.len;
-        const bool bad = BITS != 16 && !whole && __any(!(fabsf(cur.vs) < INFINITY));
+        const bool bad = BITS != 16 && __any(!(fabsf(cur.vs) < INFINITY));
         bool odd = false;
         if constexpr (BITS == 16)
             odd = !whole && cur.template odd_values<N>();
@@ -348,14 +348,20 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                 asm volatile("");  // (a branch, not a select in every tile)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (s[n][i / 4][i % 4] == -INFINITY)
-                        e[i] = 0.f;  // what an unseen position's scale holds has no influence
+                    e[i] = odd_product(s[n][i / 4][i % 4], vs[i / 4][i % 4], e[i]);
             }
             const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
             p[n] = __builtin_bit_cast(typename P::V8, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 e[i] -= (float)p[n][i];
+            if (bad) {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (fabsf((float)p[n][i]) == INFINITY)
+                        e[i] = 0.f;  // (an infinity has no rest)
+            }
             const u4 r2 = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
             rest[n] = __builtin_bit_cast(typename P::V8, r2);
         }

@@ -283,9 +283,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                         s[n][u][i] = (see >> (16 * u + i)) & 1 ? s[n][u][i] : -INFINITY;
             }
         }
-        // a scale that is not finite, and that some row does not see: what it
-        // holds has no influence there
-        const bool bad = BITS != 16 && !whole && __any(!(fabsf(vsmine) < INFINITY));
+        const bool bad = BITS != 16 && __any(!(fabsf(vsmine) < INFINITY));
         typename P::V8 p[NR][NU / 2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -329,8 +327,8 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                         asm volatile("");  // (a branch, not a select in every tile)
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (s[n][2 * h + i / 4][i % 4] == -INFINITY)
-                                e[i] = 0.f;
+                            e[i] = odd_product(s[n][2 * h + i / 4][i % 4],
+                                               sc[KT + 32 * h + 16 * (i / 4) + 4 * kq + i % 4], e[i]);
                     }
                 }
                 const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};

@@ -139,3 +139,20 @@ def test_infinite_values_far_below(lm, t, g):
             cache.v[2, 0, 9, 3] = math.inf
             out, _ = check(lm, q, cache, torch.arange(width, device="cuda", dtype=torch.int32).reshape(1, width), [n])
             assert bool(out[..., 3].isposinf().all())
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("t,g", ROWS)
+def test_infinite_scales(lm, bits, t, g):
+    """A value's scale that is infinite: infinities of the codes' signs, NaN for code zero."""
+    for dim, dtype in ((64, HF), (128, BF), (256, BF)):
+        for n in (150, 2000):
+            r = gen(t + dim)
+            page = 16
+            width = -(-(n + t) // page)
+            table = torch.randperm(width, generator=r, device="cuda").int().reshape(1, width)
+            cache = make_cache(lm, r, width, 1, page, dim, bits, dtype)
+            cache.v_scale[int(table[0, 5]), 0, 3] = math.inf
+            q = randn(r, 1, t, g, dim, dtype=dtype)
+            out, _ = check(lm, q, cache, table, [n])
+            assert bool((~torch.isfinite(out)).all())
