@@ -239,11 +239,12 @@ __device__ __forceinline__ float odd_product(float score, float scale, float pro
     return score == -INFINITY ? 0.f : fabsf(scale) == INFINITY ? scale : product;
 }
 
-// Largest exponent of the scales that lanes hold, at least -120 (zeros and what
-// is not finite do not count).
+// Largest exponent of the scales that lanes hold, of either sign, at least -120
+// (zeros and what is not finite do not count).
 template <int LANES>
 __device__ __forceinline__ int scale_exponent(float v)
 {
+    v = fabsf(v);
     int e = v > 0.f && v < INFINITY ? max(ilogbf(v), -120) : -120;
 #pragma unroll
     for (int s = 1; s < LANES; s <<= 1)

@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         const uint32_t there = cur.valid;
         if constexpr (BITS != 16) {
             // (scales that are not finite stay so)
-            if (__any(cur.vs * vscale >= 2.f && cur.vs < INFINITY)) {
+            if (__any(fabsf(cur.vs) * vscale >= 2.f && fabsf(cur.vs) < INFINITY)) {
                 const int e = scale_exponent<32>(cur.vs);
                 const float f = ldexpf(1.f, vexp - e);
 #pragma unroll

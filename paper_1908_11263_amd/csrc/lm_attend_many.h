@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
         const float vsmine = BITS == 16 ? 0.f : h.vs;
         if constexpr (BITS != 16) {
             // (scales that are not finite stay so)
-            if (__any(h.vs * vscale >= 2.f && h.vs < INFINITY)) {
+            if (__any(fabsf(h.vs) * vscale >= 2.f && fabsf(h.vs) < INFINITY)) {
                 const int e = scale_exponent<64>(h.vs);
                 const float f = ldexpf(1.f, vexp - e);
 #pragma unroll

@@ -156,3 +156,20 @@ def test_infinite_scales(lm, bits, t, g):
             q = randn(r, 1, t, g, dim, dtype=dtype)
             out, _ = check(lm, q, cache, table, [n])
             assert bool((~torch.isfinite(out)).all())
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("t,g", ROWS)
+@pytest.mark.parametrize("n", [20, 1000])
+def test_negative_scales(lm, bits, t, g, n):
+    for dim, dtype in ((64, BF), (128, HF), (256, HF)):
+        r = gen(t + dim)
+        page = 16
+        width = -(-(n + t) // page)
+        table = torch.randperm(width, generator=r, device="cuda").int().reshape(1, width)
+        cache = make_cache(lm, r, width, 1, page, dim, bits, dtype)
+        q = randn(r, 1, t, g, dim, dtype=dtype)
+        for sign in (-1.0, None):
+            for s in (cache.k_scale, cache.v_scale):
+                s *= sign or torch.where(randn(r, *s.shape) < 0, -1.0, 1.0)
+            check(lm, q, cache, table, [n])
