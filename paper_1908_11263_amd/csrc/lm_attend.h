@@ -24,8 +24,14 @@
 // rescale.  Probabilities stay below 2^(kAbove + kSlack) = 2^14, so that f16
 // holds them, and keep all its bits down to 2^-24 of the largest; sums are fp32.
 // Values of a packed cache are multiplied as f16 whatever the queries' type
-// (codes are exact there, and probabilities keep 11 bits): their scales are
-// taken relative to a power of two, the largest so far, so that they stay below 2.
+// (codes are exact there, and probabilities keep 11 bits): their scales multiply
+// the probabilities as multiples of a unit, a power of two.  Scales within
+// 2^-12 .. 2 of the unit leave a row's largest products 2^-2 and more, far above
+// f16's smallest numbers.  A tile that holds any other scale but zero (one ballot
+// a tile to see) is put off: it is added behind the loop, multiplied as bf16,
+// which has the range of fp32, each product of a probability and its scale as the
+// sum of three numbers (lm_attend_far.h).  So a scale takes no digits from a
+// position with another one, nor from a row that does not see it.
 #pragma once
 
 #include "lm_cache.h"
@@ -231,26 +237,62 @@ __device__ __forceinline__ void settle_infinities(const AttendArgs &a, const Cac
             }
 }
 
-// A probability's product with its value's scale, in a tile that holds a scale
-// that is not finite: nothing where the position is not seen, whatever it holds
-// there, and the infinity however small the probability.
-__device__ __forceinline__ float odd_product(float score, float scale, float product)
-{
-    return score == -INFINITY ? 0.f : fabsf(scale) == INFINITY ? scale : product;
-}
-
 // Largest exponent of the scales that lanes hold, of either sign, at least -120
 // (zeros and what is not finite do not count).
-template <int LANES>
 __device__ __forceinline__ int scale_exponent(float v)
 {
     v = fabsf(v);
     int e = v > 0.f && v < INFINITY ? max(ilogbf(v), -120) : -120;
 #pragma unroll
-    for (int s = 1; s < LANES; s <<= 1)
+    for (int s = 1; s < 64; s <<= 1)
         e = max(e, __shfl_xor(e, s, 64));
     return __builtin_amdgcn_readfirstlane(e);
 }
+
+// The unit of a packed cache's value scales.  Its exponent stays within 20 of 0,
+// so that products with any scale, and outputs brought from one unit to another,
+// stay within fp32.
+struct Unit {
+    static constexpr int kMost = 20;
+    int e = -kMost;
+    float inv = (float)(1 << kMost);
+
+    __device__ __forceinline__ bool out(float vs, uint64_t there) const
+    {
+        const float x = fabsf(vs) * inv;
+        return (__ballot(!(x < 2.f) || (x < 0x1p-12f && x > 0.f)) & there) != 0;
+    }
+    // Whether the tile's scales (vs: this lane's; there: lanes that hold one)
+    // are far from the unit, which rises first where they are above: the outputs
+    // so far are to be multiplied by f (1 if it does not rise).
+    __device__ __forceinline__ bool far(float vs, uint64_t there, float &f)
+    {
+        if (!out(vs, there))
+            return false;
+        asm volatile("");  // (a branch)
+        const int lane = threadIdx.x & 63;
+        const int top = min(scale_exponent((there >> lane) & 1 ? vs : 0.f), kMost);
+        if (top > e) {
+            f = ldexpf(1.f, e - top);
+            e = top;
+            inv = ldexpf(1.f, -top);
+        }
+        return out(vs, there);
+    }
+    template <int NR, int ND>
+    __device__ __forceinline__ bool far(float vs, uint64_t there, f4 (&o)[NR][ND])
+    {
+        float f = 1.f;
+        const bool is = far(vs, there, f);
+        if (f != 1.f)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    o[n][d] *= f;
+        return is;
+    }
+};
 
 hipError_t launch_attend_bf16(const AttendArgs &a, const CacheArgs &c, const AttendPlan &p, int bits, int dim,
                               hipStream_t s);

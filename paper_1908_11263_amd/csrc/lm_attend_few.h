@@ -16,7 +16,7 @@
 
 #include <type_traits>
 
-#include "lm_attend.h"
+#include "lm_attend_far.h"
 
 namespace qnn_lm {
 
@@ -196,6 +196,8 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
     const int32_t row0 = tile * 16 * NR;
     const int32_t end = sq.end(a, c, pl, row0, 16 * NR);
 
+    // the channels that K's lane loads put into product i
+    auto channel = [&](int i) { return (i / S::kSub) * 4 * S::kPiece + kq * S::kPiece + (i % S::kSub) * 8; };
     // this lane's rows: queries and draft numbers
     typename N::V8 q[NR][NK];
     int32_t draft[NR];
@@ -210,8 +212,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             draft[n] = -1;
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-            // the channels that K's lane loads put into product i
-            const int d = (i / S::kSub) * 4 * S::kPiece + kq * S::kPiece + (i % S::kSub) * 8;
+            const int d = channel(i);
             u4 v = {0, 0, 0, 0};
             if (live)
                 v = *(const u4 *)(p + d);
@@ -229,8 +230,8 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             o[n][d] = (f4){0, 0, 0, 0};
     }
     const float qs = a.scale * 1.44269504088896f * (BITS == 4 ? 1.f / 16 : 1.f);  // scores in powers of two
-    int vexp = -120;  // values' scales are taken as multiples of 2^vexp
-    float vscale = ldexpf(1.f, 120);
+    Unit unit;              // of the values' scales
+    bool put_off = false;   // tiles with scales far from it
     uint8_t *vl = lds + wave * S::kWaveLds;
     float *scales = (float *)(vl + kAttendTile * S::kPitch);
 
@@ -253,22 +254,12 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         cur.clear(lane);
         cur.stage(vl, lane);
         const uint32_t there = cur.valid;
+        bool far = false;
         if constexpr (BITS != 16) {
-            // (scales that are not finite stay so)
-            if (__any(fabsf(cur.vs) * vscale >= 2.f && fabsf(cur.vs) < INFINITY)) {
-                const int e = scale_exponent<32>(cur.vs);
-                const float f = ldexpf(1.f, vexp - e);
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-                        o[n][d] *= f;
-                vexp = e;
-                vscale = ldexpf(1.f, -e);
-            }
+            far = unit.far(cur.vs, there | (uint64_t)there << 32, o);
             if (lane < 32) {
                 scales[lane] = cur.ks * qs;
-                scales[32 + lane] = cur.vs * vscale;
+                scales[32 + lane] = cur.vs * unit.inv;
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -296,7 +287,6 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                 s[n][u] *= ks[u];
         }
         const bool whole = there == 0xFFFFFFFFu && p0 + kAttendTile <= sq.len;
-        const bool bad = BITS != 16 && __any(!(fabsf(cur.vs) < INFINITY));
         bool odd = false;
         if constexpr (BITS == 16)
             odd = !whole && cur.template odd_values<N>();
@@ -304,6 +294,10 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         const int32_t later = look(at + 12);
         load(cur, at + 8, page);
         page = later;
+        if (BITS != 16 && far) {
+            put_off = true;
+            return;
+        }
         if (!whole) {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
@@ -344,24 +338,11 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
                 if constexpr (BITS != 16)
                     e[i] *= vs[i / 4][i % 4];
             }
-            if (bad) {
-                asm volatile("");  // (a branch, not a select in every tile)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    e[i] = odd_product(s[n][i / 4][i % 4], vs[i / 4][i % 4], e[i]);
-            }
             const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
             p[n] = __builtin_bit_cast(typename P::V8, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 e[i] -= (float)p[n][i];
-            if (bad) {
-                asm volatile("");
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (fabsf((float)p[n][i]) == INFINITY)
-                        e[i] = 0.f;  // (an infinity has no rest)
-            }
             const u4 r2 = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
             rest[n] = __builtin_bit_cast(typename P::V8, r2);
         }
@@ -394,6 +375,10 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
         if (at + 4 < last)
             step(ahead[1], at + 4);
     }
+    if constexpr (BITS != 16)
+        if (put_off)
+            add_far_tiles<N, BITS, DIM, NR>(a, c, seq, head, q, draft, sq.len, first, last, 4, kAttendTile, end, qs, unit, o,
+                                            m, l, channel);
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         l[n] += __shfl_xor(l[n], 16, 64);
@@ -420,7 +405,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendArgs a, CacheArgs c, 
             top = fmaxf(top, jm[w * 16 + l16]);
         float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - top);
         if constexpr (BITS != 16)
-            f = ldexpf(f, BITS == 4 ? vexp - 4 : vexp);
+            f = ldexpf(f, BITS == 4 ? unit.e - 4 : unit.e);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
             // (a row that has seen nothing may hold anything; an infinity stays

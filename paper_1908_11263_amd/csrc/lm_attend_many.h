@@ -21,7 +21,7 @@
 
 #include <type_traits>
 
-#include "lm_attend.h"
+#include "lm_attend_far.h"
 
 namespace qnn_lm {
 
@@ -76,11 +76,11 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // row tiles of one head's piece lie eight workgroups apart: on one XCD,
     // which reads the piece from memory once
-    const int32_t unit = (int32_t)(blockIdx.x >> 3) / pl.row_tiles * 8 + (blockIdx.x & 7);
+    const int32_t work = (int32_t)(blockIdx.x >> 3) / pl.row_tiles * 8 + (blockIdx.x & 7);
     const int32_t tile = (int32_t)(blockIdx.x >> 3) % pl.row_tiles;
-    if (unit >= pl.splits * c.heads * c.b)
+    if (work >= pl.splits * c.heads * c.b)
         return;
-    const int32_t split = unit % pl.splits, head = unit / pl.splits % c.heads, seq = unit / pl.splits / c.heads;
+    const int32_t split = work % pl.splits, head = work / pl.splits % c.heads, seq = work / pl.splits / c.heads;
     const AttendSeq sq(a, seq);
     const int32_t wg0 = tile * 64 * NR, row0 = wg0 + wave * 16 * NR;
     const int32_t end = sq.end(a, c, pl, wg0, 64 * NR);
@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
             o[n][d] = (f4){0, 0, 0, 0};
     }
     const float qs = a.scale * 1.44269504088896f * (BITS == 4 ? 1.f / 16 : 1.f);
-    int vexp = -120;  // values' scales are taken as multiples of 2^vexp
-    float vscale = ldexpf(1.f, 120);
+    Unit unit;             // of the values' scales
+    bool put_off = false;  // tiles with scales far from it
 
     const int32_t tiles = (end + KT - 1) / KT;
     const int32_t share = (tiles + pl.splits - 1) / pl.splits;
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
             float *sc = (float *)(buf + 2 * KT * S::kRow);
             if (wave == 0 && lane < KT) {
                 sc[lane] = h.ks * qs;
-                sc[KT + lane] = h.vs * vscale;
+                sc[KT + lane] = h.vs * unit.inv;
             }
         }
     };
@@ -216,21 +216,9 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
         // (a lane past a tile of 32 has no position: what it has read is another's)
         if (BITS != 16 && (KT < 64 || there != S::kWhole) && !((there >> lane) & 1))
             h.ks = h.vs = 0.f;
-        const float vsmine = BITS == 16 ? 0.f : h.vs;
-        if constexpr (BITS != 16) {
-            // (scales that are not finite stay so)
-            if (__any(fabsf(h.vs) * vscale >= 2.f && fabsf(h.vs) < INFINITY)) {
-                const int e = scale_exponent<64>(h.vs);
-                const float f = ldexpf(1.f, vexp - e);
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-                        o[n][d] *= f;
-                vexp = e;
-                vscale = ldexpf(1.f, -e);
-            }
-        }
+        bool far = false;
+        if constexpr (BITS != 16)
+            far = unit.far(h.vs, there, o);
         stage(h, buf);
         // (the page numbers first: loads come back in order, and these are wanted before the tile's)
         const Pages later = look(t + S::kAhead + 1);
@@ -240,6 +228,10 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (BITS != 16 && far) {
+            put_off = true;  // (in all four waves)
+            return;
+        }
 
         const uint8_t *vb = buf + KT * S::kRow;
         const float *sc = (const float *)(buf + 2 * KT * S::kRow);
@@ -283,7 +275,6 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
                         s[n][u][i] = (see >> (16 * u + i)) & 1 ? s[n][u][i] : -INFINITY;
             }
         }
-        const bool bad = BITS != 16 && __any(!(fabsf(vsmine) < INFINITY));
         typename P::V8 p[NR][NU / 2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -322,13 +313,6 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             e[4 * u + i] *= vu[i];
-                    }
-                    if (bad) {
-                        asm volatile("");  // (a branch, not a select in every tile)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            e[i] = odd_product(s[n][2 * h + i / 4][i % 4],
-                                               sc[KT + 32 * h + 16 * (i / 4) + 4 * kq + i % 4], e[i]);
                     }
                 }
                 const u4 r = {pack2<P>(e[0], e[1]), pack2<P>(e[2], e[3]), pack2<P>(e[4], e[5]), pack2<P>(e[6], e[7])};
@@ -387,6 +371,10 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
             if (t + 1 < last)
                 step(ahead[1], t + 1);
     }
+    if constexpr (BITS != 16)
+        if (put_off)
+            add_far_tiles<N, BITS, DIM, NR>(a, c, seq, head, q, draft, sq.len, first, last, 1, KT, end, qs, unit, o, m, l,
+                                            [&](int i) { return i * 32 + kq * 8; });
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         l[n] += __shfl_xor(l[n], 16, 64);
@@ -396,7 +384,7 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
         if (any_nan<NR, ND>(o, l))
             settle_infinities<N, DIM, NR>(a, c, seq, head, draft, sq.len, first, last, 1, KT, end, o);
     const int64_t all = (int64_t)c.b * a.t * a.heads;
-    const float f = BITS == 16 ? 1.f : ldexpf(1.f, BITS == 4 ? vexp - 4 : vexp);
+    const float f = BITS == 16 ? 1.f : ldexpf(1.f, BITS == 4 ? unit.e - 4 : unit.e);
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         const int32_t row = row0 + n * 16 + l16;

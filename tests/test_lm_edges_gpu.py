@@ -173,3 +173,56 @@ def test_negative_scales(lm, bits, t, g, n):
             for s in (cache.k_scale, cache.v_scale):
                 s *= sign or torch.where(randn(r, *s.shape) < 0, -1.0, 1.0)
             check(lm, q, cache, table, [n])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("t,g", ROWS)
+@pytest.mark.parametrize("n", [20, 1000])
+def test_scales_far_apart(lm, bits, t, g, n):
+    """Values' scales from 1e-9 to 1e9 side by side, seen by every row, with scores that favour small and large ones."""
+    for dim in (64, 128, 256):
+        r = gen(t + dim)
+        page = 16
+        width = -(-(n + t) // page)
+        table = torch.randperm(width, generator=r, device="cuda").int().reshape(1, width)
+        cache = make_cache(lm, r, width, 1, page, dim, bits, BF)
+        base = randn(r, dim)
+        q = (base + 0.1 * randn(r, 1, t, g, dim)).to(BF)
+        check(lm, q, cache._replace(v_scale=cache.v_scale * 10.0 ** (18 * torch.rand(cache.v_scale.shape, generator=r, device="cuda") - 9)),
+              table, [n])
+        # one token far larger than the others, whose probability makes it smaller than they are: early, then late
+        for pos in (3, n - 2):
+            pg, slot = int(table[0, pos // page]), pos % page
+            for gap, scale in ((30, 1e6), (45, 1e10), (60, 1e18)):
+                most = 127 if bits == 8 else 7
+                want = base * (-gap * dim ** 0.5 / float(base @ base))
+                code, ks = ref.quantize(want, bits)
+                k, s, v = cache.k.clone(), cache.k_scale.clone(), cache.v_scale.clone()
+                k[pg, 0, slot] = ref.pack((code & (2 * most + 1)).to(torch.uint8), bits).cuda()
+                s[pg, 0, slot] = float(ks)
+                v[pg, 0, slot] = scale
+                check(lm, q, cache._replace(k=k, k_scale=s, v_scale=v), table, [n])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("t,g", ROWS)
+@pytest.mark.parametrize("n", [0, 20, 1000])
+def test_large_scales_of_unseen_drafts(lm, bits, t, g, n):
+    """A draft whose values are far larger than all others, and that few rows or none see: the others do not change by
+    more than sums in another order do."""
+    if t < 2:
+        return
+    for dim in (64, 128, 256):
+        r = gen(t + dim)
+        page = 16
+        width = -(-(n + t) // page)
+        table = torch.randperm(width, generator=r, device="cuda").int().reshape(1, width)
+        cache = make_cache(lm, r, width, 1, page, dim, bits, BF)
+        q = randn(r, 1, t, g, dim, dtype=BF)
+        for seen in (True, False):
+            mask = [[[j for j in range(i + 1) if j != 1 or (seen and i == 1)] for i in range(t)]]
+            pos = n + 1
+            for huge in (1e6, 1e12, 1e30):
+                v = cache.v_scale.clone()
+                v[int(table[0, pos // page]), 0, pos % page] = huge
+                check(lm, q, cache._replace(v_scale=v), table, [n], mask)
