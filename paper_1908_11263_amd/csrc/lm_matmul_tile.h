@@ -24,9 +24,12 @@
 // Group scales: the sums are kept in units of the current group's scale and
 // multiplied by the ratio of the old scale to the new one where a group ends
 // (one fp32 product, where a second set of accumulators would not fit).  A
-// group whose scale is zero, or 2^-60 of the row's largest before it, keeps the
-// unit and has its codes cleared: in units of its scale the sums would pass
-// fp32, and it adds less than fp32 resolves of what such scales stand for.
+// group whose scale is zero, or 2^-40 of the row's largest before it, keeps the
+// unit and has its codes cleared, as in units of its scale the sums could pass
+// fp32.  Where such a group holds codes after all (a quantizer that gives empty
+// groups the smallest scale there is leaves none), where a scale is 2^40 times
+// those before it, or where sums have passed fp32, the wave forms its sums anew
+// with an accumulator for each group (sums_by_groups).
 #pragma once
 
 #include "lm_matmul.h"
@@ -180,6 +183,67 @@ __device__ __forceinline__ void interleave()
     }
 }
 
+// Scales that are this many times apart are not brought to one another's unit.
+constexpr float kApart = 0x1p40f;
+
+// Whether clearing groups, or bringing the sums before one to its unit, has lost
+// something of a row: a group of codes that are not all zero, a scale 1 / kApart
+// of an earlier one, or codes before a scale kApart times theirs.
+template <int BITS>
+__device__ __forceinline__ bool groups_lost(const uint8_t *w, const float *scale, int32_t first, int32_t last, int32_t group)
+{
+    auto empty = [&](int32_t g) {
+        if (BITS == 1)
+            return false;  // (there is no code of zero)
+        const uint8_t *p = w + (int64_t)g * group * BITS / 8;
+        uint32_t any = 0;
+        for (int i = 0; i < group * BITS / 8; i += 8) {
+            const u2 v = *(const u2 *)(p + i);
+            any |= v.x | v.y;
+        }
+        return any == 0;
+    };
+    float top = 0.f;
+#pragma unroll 1
+    for (int32_t g = first; g < last; ++g) {
+        const float s = __builtin_fabsf(scale[g]);
+        if (s == 0.f)
+            continue;
+        if (s * kApart < top && !empty(g))
+            return true;
+        if (top != 0.f && top * kApart < s)
+            for (int32_t e = first; e < g; ++e)
+                if (scale[e] != 0.f && !empty(e))
+                    return true;
+        top = fmaxf(top, s);
+    }
+    return false;
+}
+
+// The sums of a block of 32 rows of x by 32 of weights (x, w: this lane's rows)
+// over groups first to last, each group's products in an accumulator of its own:
+// straight from memory, for weights whose scales lie far apart.
+template <class N, int BITS>
+__device__ __forceinline__ f16v sums_by_groups(const typename N::T *x, const uint8_t *w, const float *scale, int32_t first,
+                                               int32_t last, int32_t group, int half)
+{
+    f16v sum = {};
+#pragma unroll 1
+    for (int32_t g = first; g < last; ++g) {
+        f16v part = {};
+#pragma unroll 1
+        for (int32_t k = g * group + 16 * half; k < (g + 1) * group; k += 32)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                uint32_t raw[2] = {0, 0};
+                load_raw<BITS>(w + (int64_t)(k + 8 * f) * BITS / 8, raw);
+                part = mfma32(*(const typename N::V8 *)(x + k + 8 * f), expand<N, BITS, 0>(raw), part);
+            }
+        sum += part * scale[g];
+    }
+    return sum;
+}
+
 template <class N, int BITS, int TF, int WF, int GPB, bool GATED>
 __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileGrid g)
 {
@@ -302,9 +366,10 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 acc[m][n][i] = 0.f;
     float unit[WF], top[WF];  // the sums' unit, the largest scale so far
     uint32_t clear[WF];       // 0 where the group's codes count
+    uint32_t low[WF];         // the smallest but zero, by bits: twice them without the sign, less one
 #pragma unroll
     for (int n = 0; n < WF; ++n)
-        unit[n] = 1.f, top[n] = 0.f, clear[n] = 0;
+        unit[n] = 1.f, top[n] = 0.f, clear[n] = 0, low[n] = 0xFFFFFFFFu;
 
     const int32_t steps = min(begin + g.steps, (a.k + S::KS - 1) / S::KS);
     constexpr int BLOCKS = S::KS / 32;
@@ -360,7 +425,8 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
                 const int at = !GATED ? (wave * WF + n) * 32 + l32
                                : WF == 2 ? n * 128 + wave * 32 + l32 : (l32 >> 4) * 64 + wave * 16 + (l32 & 15);
                 const float sc = ss[at * 4 + (group & 3) + max(0, 4 * quad - sleft[n])];
-                const bool small = __builtin_fabsf(sc) * 0x1p60f < top[n] || sc == 0.f;
+                const bool small = __builtin_fabsf(sc) * kApart < top[n] || sc == 0.f;
+                low[n] = min(low[n], 2 * __float_as_uint(sc) - 1);
                 clear[n] = small ? 0xFFFFFFFFu : 0;
                 f[b][n] = small || top[n] == 0.f ? 1.f : unit[n] / sc;  // (no sums yet)
                 unit[n] = small ? unit[n] : sc;
@@ -512,6 +578,45 @@ __global__ void __launch_bounds__(256, 2) matmul_tile_kernel(MatmulArgs a, TileG
             } else {
                 products<N, TF, WF>(ahead[0][0], acc);
                 products<N, TF, WF>(ahead[0][1], acc);
+            }
+        }
+    }
+    if constexpr (GPB != 0) {
+        bool apart = false, passed = false;  // scales far apart; sums that are not finite
+#pragma unroll
+        for (int n = 0; n < WF; ++n)
+            apart |= __uint_as_float((low[n] >> 1) + 1) * kApart < top[n];
+#pragma unroll
+        for (int m = 0; m < TF; ++m)
+#pragma unroll
+            for (int n = 0; n < WF; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    passed |= !(__builtin_fabsf(acc[m][n][i]) < INFINITY);
+        if (__any(apart || passed)) {
+            const uint8_t *w[WF];
+            const float *scale[WF];
+            const int32_t g0 = (begin * S::KS) >> gshift, g1 = (min(steps * S::KS, a.k) + a.group - 1) >> gshift;
+#pragma unroll
+            for (int n = 0; n < WF; ++n) {
+                const int q = n * 32 + l32;  // row of this wave
+                const int32_t j = min(j0 + (GATED ? wave * GR + q % HR : wave * WF * 32 + q), a.m - 1);
+                const int64_t row = GATED && q >= GR ? (int64_t)a.m + j : j;
+                w[n] = (const uint8_t *)a.w + row * a.w_row;
+                scale[n] = a.scale + row * a.groups;
+                passed |= apart && groups_lost<BITS>(w[n], scale[n], g0, g1, a.group);
+            }
+            if (__any(passed)) {
+#pragma unroll
+                for (int m = 0; m < TF; ++m) {
+                    const typename N::T *x = (const typename N::T *)a.x + min(r0 + m * 32 + l32, a.r - 1) * a.x_pitch;
+#pragma unroll
+                    for (int n = 0; n < WF; ++n)
+                        acc[m][n] = sums_by_groups<N, BITS>(x, w[n], scale[n], g0, g1, a.group, half);
+                }
+#pragma unroll
+                for (int n = 0; n < WF; ++n)
+                    unit[n] = 1.f;
             }
         }
     }

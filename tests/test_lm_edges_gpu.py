@@ -226,3 +226,60 @@ def test_large_scales_of_unseen_drafts(lm, bits, t, g, n):
                 v = cache.v_scale.clone()
                 v[int(table[0, pos // page]), 0, pos % page] = huge
                 check(lm, q, cache._replace(v_scale=v), table, [n], mask)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 2, 1])
+@pytest.mark.parametrize("r", [5, 24, 70, 300])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_group_scales_in_any_order(lm, bits, r, group):
+    """Scales more than 2^60 apart, the large one first, last or between, where x is zero in the columns of the large
+    one; and numbers of x that bring a group's sums near the end of 32 bits."""
+    for gated in (False, True):
+        g = gen(bits + r)
+        L = layer(g, r, 1280, 150, bits, group, BF, gated)
+        n = 1280 // group
+        for at in (0, n // 2, n - 1):
+            x, s = L["x"].clone(), torch.full_like(L["scale"], 2.0 ** -75)
+            s[:, at] = 1.0
+            x[:, at * group:(at + 1) * group] = 0
+            if r > 1:
+                x[1] = L["x"][1]  # one row that the large group counts for
+            act = "relu" if gated else "none"
+            y = lm.matmul(x, L["w"], bits, scale=s, act=act, gated=gated)
+            want, bound = ref.matmul(x, L["w"], bits, s, None, act, gated)
+            ref.close(y, want, bound, "at %d" % at)
+            if gated:
+                continue
+            x, s = L["x"].clone(), torch.full_like(L["scale"], 2.0 ** -58)
+            s[:, at] = 1.0
+            x[:, at * group:(at + 1) * group] *= 1e25
+            y = lm.matmul(x, L["w"], bits, scale=s)
+            want, bound = ref.matmul(x, L["w"], bits, s)
+            ref.close(y, want, bound, "large x at %d" % at)
+
+
+@pytest.mark.parametrize("bits,group", [(8, 128), (4, 64), (4, 32), (2, 128), (1, 32)])
+@pytest.mark.parametrize("r", [2033, 1003])
+def test_group_scales_in_large_tiles(lm, bits, group, r):
+    """The same in tiles of 128 x 256 and of 64 x 256: a few rows of weights, and a few of x, are the odd ones."""
+    g = gen(bits + r)
+    L = layer(g, r, 512, 8001, bits, group, BF)
+    x, s = L["x"], L["scale"]
+    s[1000] = 2.0 ** -75
+    s[1000, -1], s[4000, 0] = 1.0, 2.0 ** 70
+    x[7, 512 - group:] = 0
+    x[:4, :group] = 0
+    x[11, :group] *= 1e25
+    want, bound = ref.matmul(x, L["w"], bits, s)
+    # (row 4000's results for the large x pass the type)
+    most = torch.finfo(BF).max * (1 + 2.0 ** -9)
+    want = torch.where(want.abs() >= most, want.sign() * math.inf, want)
+    ref.close(lm.matmul(x, L["w"], bits, scale=s), want, bound, "large tiles")
+    # rows of nothing but the smallest scale and codes of zero (the lowest codes at one bit) in every second group
+    if bits > 1:
+        s = torch.full_like(s, 2.0 ** -4)
+        s[:, ::2] = 1e-45
+        w = L["w"].reshape(8001, -1, group * bits // 8).clone()
+        w[:, ::2] = 0
+        w = w.reshape(8001, -1)
+        ref.close(lm.matmul(L["x"], w, bits, scale=s), *ref.matmul(L["x"], w, bits, s), "empty groups")
