@@ -99,8 +99,12 @@ def tree_step(h, first_norm, blocks, caches, table, lens, mask=None, counts=None
 def accept_path(caches, table, lens, path, kept, stream=None):
     """After the drafts of a step have been judged: the accepted ones (path, kept
     as lm.cache_keep takes them) become the tokens behind lens in every block's
-    cache.  Returns the new lens."""
+    cache.  Returns the new lens, like them computed on `stream`."""
     from . import lm
+    if stream is not None:
+        import torch
+        with torch.cuda.stream(stream):
+            return accept_path(caches, table, lens, path, kept)
     for cache in caches:
-        lm.cache_keep(cache, table, lens, path, kept, stream=stream)
+        lm.cache_keep(cache, table, lens, path, kept)
     return lens + kept
