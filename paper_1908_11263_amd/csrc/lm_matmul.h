@@ -6,18 +6,23 @@
 
 namespace qnn_lm {
 
-// t Phi(t) from erfc x = p(u) exp(-x^2), u = 1 / (1 + 0.3275911 x), x = |t| / sqrt 2
-// (Abramowitz and Stegun, 7.1.26: erf within 1.5e-7, the result within 1.1e-7 (1 +
-// |t|) and, for |t| < 5, 0.2 % of itself, as nothing cancels below 0): a third of
-// erff's instructions (1777 x 2080 to 6001 at 8 bits: 78 us against 85).
+// t Phi(t) from erfc x = p(u) exp(-x^2), u = 1 / (1 + 0.425 x), x = |t| / sqrt 2:
+// p without a constant, of degree 8, is fitted to erfc's scaled form so that its
+// largest relative error over 0 .. 9.6 is least (1.3e-7, found by weighted least
+// squares).  Nothing cancels below 0: the result is within 3e-6 of itself for |t|
+// < 5 and 1e-5 for |t| < 9, where the exponential's argument rounds, far below its
+// own rounding to 16 bits.  (t / 2 (1 + erf) in 32 bits is off by 3e-4 at -3.5.)
 __device__ __forceinline__ float gelu(float t)
 {
     const float x = __builtin_fabsf(t) * 0.707106781186548f;
-    const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
-    float p = __builtin_fmaf(1.061405429f, u, -1.453152027f);
-    p = __builtin_fmaf(p, u, 1.421413741f);
-    p = __builtin_fmaf(p, u, -0.284496736f);
-    p = __builtin_fmaf(p, u, 0.254829592f);
+    const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.425f, x, 1.f));
+    float p = __builtin_fmaf(0.0720406324f, u, -0.315499127f);
+    p = __builtin_fmaf(p, u, 0.41165176f);
+    p = __builtin_fmaf(p, u, -0.106962503f);
+    p = __builtin_fmaf(p, u, 0.25704947f);
+    p = __builtin_fmaf(p, u, 0.200111344f);
+    p = __builtin_fmaf(p, u, 0.241935894f);
+    p = __builtin_fmaf(p, u, 0.239672408f);
     const float q = 0.5f * p * u * __builtin_amdgcn_exp2f(x * x * -1.44269504088896f);  // Phi(-|t|)
     return t * (t > 0.f ? 1.f - q : q);
 }
