@@ -32,8 +32,8 @@ hipError_t launch_many(const AttendArgs &a, const CacheArgs &c, const AttendPlan
     constexpr size_t lds = 2 * ManyShape<BITS, DIM>::kBuffer;
     static std::atomic<uint64_t> devices{0};
     attend_lds(attend_many_kernel<N, BITS, DIM, NR>, lds, devices);
-    const unsigned units = ((unsigned)p.splits * c.heads * c.b + 7) / 8 * 8;
-    hipLaunchKernelGGL((attend_many_kernel<N, BITS, DIM, NR>), dim3(units * p.row_tiles), dim3(256), lds, s, a, c, p);
+    const int64_t units = ((int64_t)p.splits * c.heads * c.b + 7) / 8 * 8;
+    hipLaunchKernelGGL((attend_many_kernel<N, BITS, DIM, NR>), grid_of(units * p.row_tiles), dim3(256), lds, s, a, c, p);
     return hipGetLastError();
 }
 

@@ -76,8 +76,9 @@ __global__ void __launch_bounds__(256, (ManyShape<BITS, DIM>::groups(NR))) atten
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // row tiles of one head's piece lie eight workgroups apart: on one XCD,
     // which reads the piece from memory once
-    const int32_t work = (int32_t)(blockIdx.x >> 3) / pl.row_tiles * 8 + (blockIdx.x & 7);
-    const int32_t tile = (int32_t)(blockIdx.x >> 3) % pl.row_tiles;
+    const int32_t group = workgroup();
+    const int32_t work = (group >> 3) / pl.row_tiles * 8 + (group & 7);
+    const int32_t tile = (group >> 3) % pl.row_tiles;
     if (work >= pl.splits * c.heads * c.b)
         return;
     const int32_t split = work % pl.splits, head = work / pl.splits % c.heads, seq = work / pl.splits / c.heads;

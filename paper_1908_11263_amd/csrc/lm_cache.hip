@@ -102,7 +102,7 @@ template <class N, int BITS, int DIM>
 __global__ void __launch_bounds__(256) append_kernel(CacheArgs c, TokenArgs a)
 {
     constexpr int LANES = DIM / 8;
-    const uint32_t n = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const uint32_t n = workgroup() * (256 / LANES) + threadIdx.x / LANES;
     const int lane = threadIdx.x % LANES;
     if (n >= a.tokens)
         return;
@@ -150,7 +150,7 @@ template <class N, class C, int BITS, int DIM>
 __global__ void __launch_bounds__(256) read_kernel(CacheArgs c, ReadArgs a)
 {
     constexpr int LANES = DIM / 8;
-    const uint32_t n = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const uint32_t n = workgroup() * (256 / LANES) + threadIdx.x / LANES;
     const int lane = threadIdx.x % LANES;
     if (n >= a.tokens)
         return;
@@ -242,7 +242,7 @@ template <class N, int BITS>
 static hipError_t append_bits(const CacheArgs &c, int dim, const TokenArgs &a, hipStream_t s)
 {
 #define CALL(D)                                                                                              \
-    hipLaunchKernelGGL((append_kernel<N, BITS, D>), dim3((a.tokens + 2048 / D - 1) / (2048 / D)), dim3(256), 0, s, c, a); \
+    hipLaunchKernelGGL((append_kernel<N, BITS, D>), grid_of((a.tokens + 2048 / D - 1) / (2048 / D)), dim3(256), 0, s, c, a); \
     break;
     QNN_LM_DIMS(CALL)
 #undef CALL
@@ -276,7 +276,7 @@ template <class N, class C, int BITS>
 static hipError_t read_bits(const CacheArgs &c, int dim, const ReadArgs &a, hipStream_t s)
 {
 #define CALL(D)                                                                                              \
-    hipLaunchKernelGGL((read_kernel<N, C, BITS, D>), dim3((a.tokens + 2048 / D - 1) / (2048 / D)), dim3(256), 0, s, c, a); \
+    hipLaunchKernelGGL((read_kernel<N, C, BITS, D>), grid_of((a.tokens + 2048 / D - 1) / (2048 / D)), dim3(256), 0, s, c, a); \
     break;
     QNN_LM_DIMS(CALL)
 #undef CALL

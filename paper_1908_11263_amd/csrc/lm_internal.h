@@ -9,6 +9,16 @@
 
 namespace qnn_lm {
 
+// A launch may have fewer than 2^32 threads along an axis: more than 2^20
+// workgroups are laid out in rows of so many, and a kernel takes its number from
+// workgroup().  The last row's may lie past the end.
+inline dim3 grid_of(int64_t groups)
+{
+    const int64_t row = 1 << 20;
+    return groups <= row ? dim3((unsigned)groups) : dim3((unsigned)row, (unsigned)((groups + row - 1) / row));
+}
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 struct MatmulArgs {
     const void *x, *w, *residual;
     const float *scale, *bias;

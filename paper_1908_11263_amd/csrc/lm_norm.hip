@@ -119,8 +119,8 @@ template <class N, class H, int WAVES, int VEC, int NV>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(NormArgs a)
 {
     __shared__ float red[WAVES];
-    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    if (WAVES == 1 && row >= a.r)
+    const int64_t row = WAVES == 1 ? (int64_t)workgroup() * 4 + (threadIdx.x >> 6) : workgroup();
+    if (row >= a.r)
         return;
     float h[NV][VEC], z[NV][VEC];
 #pragma unroll
@@ -174,8 +174,8 @@ hipError_t launch_sized(const NormArgs &a, hipStream_t s)
     const int64_t vecs = (a.d + VEC - 1) / VEC;  // of a row
 #define QNN_LM_NORM(WAVES, NV)                                                                                     \
     if (vecs <= (WAVES) * 64 * (NV)) {                                                                             \
-        const unsigned grid = (WAVES) == 1 ? (unsigned)((a.r + 3) / 4) : (unsigned)a.r;                            \
-        hipLaunchKernelGGL((norm_kernel<N, H, WAVES, VEC, NV>), dim3(grid), dim3((WAVES) == 1 ? 256 : (WAVES) * 64), \
+        const dim3 grid = grid_of((WAVES) == 1 ? ((int64_t)a.r + 3) / 4 : a.r);                                    \
+        hipLaunchKernelGGL((norm_kernel<N, H, WAVES, VEC, NV>), grid, dim3((WAVES) == 1 ? 256 : (WAVES) * 64),       \
                            0, s, a);                                                                               \
         return hipGetLastError();                                                                                  \
     }
