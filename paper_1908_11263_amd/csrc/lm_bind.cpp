@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -49,7 +50,11 @@ const Tensor &tensor(PyObject *o, const char *what)
 {
     if (!THPVariable_Check(o))
         bad(std::string(what) + " must be a tensor");
-    return THPVariable_Unpack(o);
+    const Tensor &t = THPVariable_Unpack(o);
+    // (a result without a gradient would look like one that has none)
+    if (t.requires_grad() && at::GradMode::is_enabled())
+        bad(std::string(what) + " requires a gradient, which these operators do not have: call them under torch.no_grad()");
+    return t;
 }
 
 const Tensor *maybe(PyObject *o, const char *what) { return o == Py_None ? nullptr : &tensor(o, what); }
