@@ -12,6 +12,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
+#include <ATen/ops/clone.h>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -19,6 +20,7 @@
 
 #include <stdexcept>
 #include <string>
+#include <vector>
 
 #include "qnn_lm.h"
 
@@ -74,6 +76,7 @@ int type16_of(at::ScalarType t)
 // current one (or, with no device at all, on the host: the library refuses).
 struct Place {
     at::Device device;
+    std::vector<Tensor> copies;
     explicit Place(const Tensor &t) : device(t.device()) {}
     void same(const Tensor &t) const
     {
@@ -101,14 +104,23 @@ struct Place {
         same(*t);
         return (const float *)t->data_ptr();
     }
-    const int32_t *ints(const Tensor *t, int64_t n, const char *what) const
+    // Lengths, page numbers, paths and masks may be slices of larger tensors (a
+    // part of a batch): what the library's alignment refuses is copied.
+    const void *whole(const Tensor &t)
+    {
+        if (((uintptr_t)t.data_ptr() & 15u) == 0)
+            return t.data_ptr();
+        copies.push_back(t.clone());
+        return copies.back().data_ptr();
+    }
+    const int32_t *ints(const Tensor *t, int64_t n, const char *what)
     {
         if (!t)
             return nullptr;
         if (t->scalar_type() != at::kInt || t->dim() != 1 || t->numel() != n || !t->is_contiguous())
             bad(std::string(what) + " must be contiguous int32 of " + std::to_string(n));
         same(*t);
-        return (const int32_t *)t->data_ptr();
+        return (const int32_t *)whole(*t);
     }
 };
 
@@ -368,7 +380,7 @@ struct Cache {
     qnn_lm_cache c;
     at::ScalarType type;  // of the numbers at 16 bits
 
-    Cache(PyObject *o, PyObject *t, int64_t b, const Place &at)
+    Cache(PyObject *o, PyObject *t, int64_t b, Place &at)
     {
         if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 5)
             bad("a cache is a lm.Cache");
@@ -420,7 +432,7 @@ struct Cache {
         c.v_slot = v.stride(2) * unit;
         c.k = data(k);
         c.v = data(v);
-        c.table = (const int32_t *)data(table);
+        c.table = (const int32_t *)at.whole(table);
         c.b = int32_of(b, "the number of sequences");
         c.width = int32_of(table.size(1), "the table");
     }
@@ -436,7 +448,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (q.dim() != 4 || q.stride(3) != 1)
             bad("q must be [b, t, heads, dim], contiguous along dim");
         const int64_t b = q.size(0), t = q.size(1), dim = q.size(3);
-        const Place at(q);
+        Place at(q);
         const Cache cache(a[1], a[2], b, at);
         qnn_lm_queries s;
         s.type = type16_of(q.scalar_type());
@@ -473,9 +485,9 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         const size_t size = g_lib.tree_attention_workspace(&s, &cache.c);
         if (size)
             ws = make({(int64_t)size}, q, at::kByte);
-        check(g_lib.tree_attention(&s, data(q), &cache.c, lens, counts, mask ? (const uint64_t *)data(*mask) : nullptr,
-                                   data(given ? *given : made), want ? (float *)data(lse) : nullptr,
-                                   size ? data(ws) : nullptr, size, stream),
+        check(g_lib.tree_attention(&s, data(q), &cache.c, lens, counts,
+                                   mask ? (const uint64_t *)at.whole(*mask) : nullptr, data(given ? *given : made),
+                                   want ? (float *)data(lse) : nullptr, size ? data(ws) : nullptr, size, stream),
               "qnn_lm_tree_attention");
         PyObject *out = given ? own(a[7]) : THPVariable_Wrap(made);
         return want ? pair(out, THPVariable_Wrap(lse)) : out;
@@ -493,7 +505,7 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (k.stride(3) != 1 || v.stride(3) != 1)
             bad("k and v must be contiguous along dim");
         const int64_t b = k.size(0);
-        const Place at(k);
+        Place at(k);
         const Cache cache(a[2], a[3], b, at);
         qnn_lm_tokens s;
         s.type = type16_of(k.scalar_type());
@@ -523,11 +535,11 @@ PyObject *cache_keep(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (path.scalar_type() != at::kInt || path.dim() != 2 || !path.is_contiguous())
             bad("path must be contiguous int32 [b, t]");
         const int64_t b = path.size(0);
-        const Place at(path);
+        Place at(path);
         const Cache cache(a[0], a[1], b, at);
         const int32_t *lens = at.ints(&tensor(a[2], "lens"), b, "lens"), *kept = at.ints(&tensor(a[4], "kept"), b, "kept");
-        check(g_lib.cache_keep(&cache.c, int32_of(path.size(1), "the number of drafts"), lens, (const int32_t *)data(path),
-                               kept, at.stream()),
+        check(g_lib.cache_keep(&cache.c, int32_of(path.size(1), "the number of drafts"), lens,
+                               (const int32_t *)at.whole(path), kept, at.stream()),
               "qnn_lm_cache_keep");
         return own(Py_None);
     });
@@ -544,7 +556,7 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
         const long type = number(a[4]);
         if (type < 0 || type > 2 || t < 0)
             bad("n must not be negative, dtype bfloat16, float16 or float32");
-        const Place at(start);
+        Place at(start);
         const Cache cache(a[0], a[1], b, at);
         const int32_t *from = at.ints(&start, b, "start");
         void *stream = at.stream();

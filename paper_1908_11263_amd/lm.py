@@ -5,12 +5,14 @@ Argument marshalling only, as in qnn.py: every computation runs in the
 library's HIP kernels, there is no fallback.  The marshalling itself is compiled
 (csrc/lm_bind.cpp): a call of a small layer takes a few microseconds on the
 device, and looking at its tensors from Python takes longer.  Tensors live on
-the current HIP device; work is enqueued on torch's current stream or on `stream`, and what a
-call allocates (its result, its workspace) belongs to that stream.  What the
-library can check it refuses with QnnError; what only the binding can see (a
-tensor's type, shape, strides, device) raises ValueError.  The operators are
-forward only: a tensor that requires a gradient is refused while torch records
-them (torch.no_grad() says that none is meant).
+the current HIP device; work is enqueued on torch's current stream or on
+`stream`, and what a call allocates (its result, its workspace) belongs to that
+stream.  Tensors start on 16 bytes; lengths, counts, tables, masks and paths that
+do not (lens[1:], a part of a batch) are copied.  What the library can check it
+refuses with QnnError; what only the binding can see (a tensor's type, shape,
+strides, device) raises ValueError.  The operators are forward only: a tensor
+that requires a gradient is refused while torch records them (torch.no_grad()
+says that none is meant).
 
 A cache is a `Cache`: k and v are [pages, heads, page, dim] tensors of 16-bit
 numbers (bits = 16), or uint8 tensors whose last axis holds dim codes of 8 or 4
