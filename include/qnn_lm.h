@@ -78,8 +78,8 @@ typedef struct {
  * floats, NULL (and only then) at 16 bits.  bias: [rows] floats or NULL.
  * residual may be NULL and may be y itself.  ws: at least
  * qnn_lm_matmul_workspace(s) bytes, or NULL where that is 0; its contents need
- * not be set and are not kept.  Limits: k <= 2^20, rows of weights and
- * of x <= 2^24, each tensor < 2^40 bytes.
+ * not be set and are not kept.  Limits: k <= 2^20, rows of weights <= 2^24 (of
+ * both halves together), rows of x <= 2^21, each tensor < 2^40 bytes.
  */
 qnn_status qnn_lm_matmul(const qnn_lm_linear *s, const void *x, const void *w, const float *scale,
                          const float *bias, const void *residual, void *y, void *ws, size_t ws_bytes,
@@ -120,7 +120,8 @@ qnn_status qnn_lm_norm_residual(const qnn_lm_norms *s, const void *h, const void
  * multiples of 16 (a 4-bit slot of 64 channels: 32 bytes); the channels of a
  * slot are contiguous.  Codes are symmetric (-(2^(bits-1) - 1) to its
  * opposite as written by qnn_lm_cache_append; any code is read), a value is
- * code * scale[page][head][slot].
+ * code * scale[page][head][slot].  Limits: width * page <= 2^31 - 256, b <=
+ * 65535, heads <= 32767; of a call's tokens, 2 * b * t * heads <= 2^31 - 256.
  */
 typedef struct {
     int32_t type;    /* of the numbers at 16 bits: QNN_LM_BF16 or QNN_LM_F16 */
@@ -148,7 +149,8 @@ typedef struct {
  *   out:    [b][t][heads][dim] `type` numbers; lse: [b][t][heads] floats, the
  *           natural logarithm of the sum of exponentials, or NULL.
  * A draft that sees nothing, and one at or past its count, gets zeros and
- * -infinity.  What an unseen position holds has no influence.
+ * -infinity.  What an unseen position holds has no influence.  Limits: t * heads
+ * <= 2^24, b * t * heads <= 2^31 - 256.
  */
 typedef struct {
     int32_t type;   /* of q and out (at 16 bits the cache's type) */
