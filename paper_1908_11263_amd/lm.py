@@ -65,8 +65,16 @@ class _Unloaded:
 _bind = _Unloaded()
 
 
-def _on(stream):
-    """Makes `stream` the current one for a call, so that what it allocates is the stream's."""
+def _on(stream, *tensors):
+    """Makes `stream` the current one for a call, so that what it allocates is the
+    stream's, and tells the allocator that the stream uses the call's tensors: a
+    caller may drop them when the call returns."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor):
+            if t.is_cuda:
+                t.record_stream(stream)
+        elif isinstance(t, Cache):
+            _on(stream, *t)
     return torch.cuda.stream(stream)
 
 
@@ -80,7 +88,7 @@ def matmul(x, w, bits, scale=None, bias=None, act="none", gated=False, residual=
     float32 [rows] or [rows, groups], k / groups being 32, 64 or 128.  bias:
     float32 [rows].  Returns [..., m] of x's type; out may be residual."""
     if stream is not None:
-        with _on(stream):
+        with _on(stream, x, w, scale, bias, residual, out):
             return matmul(x, w, bits, scale, bias, act, gated, residual, out)
     return _bind.matmul(x, w, bits, scale, bias, _ACTS[act], gated, residual, out)
 
@@ -98,7 +106,7 @@ def norm_residual(h, y=None, norm="rms", post=True, post_weight=None, post_bias=
     [gates, d] of y's type, each row for as many consecutive rows of y.  h_out
     may be h, out may be y."""
     if stream is not None:
-        with _on(stream):
+        with _on(stream, h, y, post_weight, post_bias, pre_weight, pre_bias, gate, h_out, out):
             return norm_residual(h, y, norm, post, post_weight, post_bias, pre_weight, pre_bias, gate, alpha, beta, eps,
                                  dtype, h_out, out)
     like = torch.empty(0, dtype=dtype) if dtype is not None and y is None else None
@@ -128,7 +136,7 @@ def tree_attention(q, cache, table, lens, mask=None, counts=None, scale=None, ou
     not given.  Returns [b, t, heads, dim], with want_lse also float32
     [b, t, heads]."""
     if stream is not None:
-        with _on(stream):
+        with _on(stream, q, cache, table, lens, mask, counts, out):
             return tree_attention(q, cache, table, lens, mask, counts, scale, out, want_lse)
     return _bind.tree_attention(q, cache, table, lens, mask, counts, q.shape[-1] ** -0.5 if scale is None else scale, out,
                                 want_lse)
@@ -139,7 +147,7 @@ def cache_append(k, v, cache, table, lens, counts=None, stream=None):
     [b, t, heads, dim] bfloat16 or float16, token j of a sequence to position
     lens + j where j < counts (None: t)."""
     if stream is not None:
-        with _on(stream):
+        with _on(stream, k, v, cache, table, lens, counts):
             return cache_append(k, v, cache, table, lens, counts)
     return _bind.cache_append(k, v, cache, table, lens, counts)
 
@@ -149,7 +157,7 @@ def cache_keep(cache, table, lens, path, kept, stream=None):
     lens + j takes position lens + path[:, j] for j < kept.  path: int32 [b, t],
     strictly ascending; kept: int32 [b]."""
     if stream is not None:
-        with _on(stream):
+        with _on(stream, cache, table, lens, path, kept):
             return cache_keep(cache, table, lens, path, kept)
     return _bind.cache_keep(cache, table, lens, path, kept)
 
@@ -159,6 +167,6 @@ def cache_read(cache, table, start, n, dtype=torch.bfloat16, stream=None):
     (qnn_lm_cache_read): (k, v), each [b, n, heads, dim] of `dtype`; zeros where
     the table does not reach."""
     if stream is not None:
-        with _on(stream):
+        with _on(stream, cache, table, start):
             return cache_read(cache, table, start, n, dtype)
     return _bind.cache_read(cache, table, start, n, _TYPES.get(dtype, -1))

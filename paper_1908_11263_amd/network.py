@@ -102,8 +102,7 @@ def accept_path(caches, table, lens, path, kept, stream=None):
     cache.  Returns the new lens, like them computed on `stream`."""
     from . import lm
     if stream is not None:
-        import torch
-        with torch.cuda.stream(stream):
+        with lm._on(stream, *caches, table, lens, path, kept):
             return accept_path(caches, table, lens, path, kept)
     for cache in caches:
         lm.cache_keep(cache, table, lens, path, kept)

@@ -57,3 +57,31 @@ def test_steps_on_a_side_stream():
     assert got[1][1].tolist() == [43, 19]
     for x, y in zip(*got):
         assert torch.equal(x, y)
+
+
+def test_arguments_dropped_at_once():
+    """Arguments made for a call on a side stream and dropped when it returns: their memory is not given to others
+    before the side stream has read them."""
+    from paper_1908_11263_amd import lm
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x = torch.randn((512, 1024), generator=g, device="cuda").to(BF)
+    w = torch.randn((256, 1024), generator=g, device="cuda").to(BF)
+    want, (_, normed) = lm.matmul(x, w, 16), lm.norm_residual(x, x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        busy()
+    torch.cuda.synchronize()  # (what busy() compiles or loads has been)
+    got = []
+    for call in (lambda v: lm.matmul(v, w, 16, stream=side), lambda v: lm.norm_residual(v, x, stream=side)[1]):
+        copy = x.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            busy()
+        got.append(call(copy))
+        del copy
+        others = [torch.full_like(x, float("nan")) for _ in range(4)]
+        torch.cuda.synchronize()
+        del others
+    assert torch.equal(got[0], want) and torch.equal(got[1], normed)
