@@ -170,7 +170,10 @@ template <class N, class H, int VEC>
 hipError_t launch_sized(const NormArgs &a, hipStream_t s)
 {
     // A wave a row up to 1024 elements (16-byte accesses), a workgroup a row
-    // above: the fewest registers that hold the row.
+    // above: the fewest registers that hold the row.  One element an access: 8
+    // or 32 a thread, the 32 of sixteen waves only (four waves with 32 went to
+    // scratch memory: 4000 rows of 7287 4657 us, with sixteen and 8 126; of 7288
+    // 79).
     const int64_t vecs = (a.d + VEC - 1) / VEC;  // of a row
 #define QNN_LM_NORM(WAVES, NV)                                                                                     \
     if (vecs <= (WAVES) * 64 * (NV)) {                                                                             \
@@ -188,7 +191,7 @@ hipError_t launch_sized(const NormArgs &a, hipStream_t s)
         QNN_LM_NORM(16, 4)
     } else {
         QNN_LM_NORM(4, 8)
-        QNN_LM_NORM(4, 32)
+        QNN_LM_NORM(16, 8)
         QNN_LM_NORM(16, 32)
     }
 #undef QNN_LM_NORM
