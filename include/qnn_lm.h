@@ -22,10 +22,13 @@
  * softmax statistics, norms and epilogues are kept in 32-bit floating point;
  * results are rounded once, to nearest even, when they are stored.  The
  * attention's probabilities multiply the values as 16-bit numbers, each off by
- * 2^-12 of itself at most (2^-9 over a cache of bf16 numbers); with up to 32 rows
- * a cache head (16 of 256 channels) as the sum of two such numbers.  Their own
- * sum is not rounded.  The order of every sum is fixed: the same call gives the
- * same bits.
+ * 2^-12 of itself or 2^-35 of the row's largest at most (2^-9 of itself over a
+ * cache of bf16 numbers); with up to 32 rows a cache head (16 of 256 channels) as
+ * the sum of two such numbers, and next to value scales more than 2^12 apart as
+ * the sum of three bf16 numbers.  Their own sum is not rounded.  The order of
+ * every sum is fixed: the same call gives the same bits.
+ * NaN and infinities that enter a sum come out of it as of the formula; scales
+ * may have either sign.
  * Values that live on the device (lengths, page numbers, paths) cannot be
  * checked on the host.  The kernels bound every index that they make of them:
  * a position whose page number is outside of the cache, or that the table does
@@ -148,9 +151,9 @@ typedef struct {
  *           drafts 0 .. i.
  *   out:    [b][t][heads][dim] `type` numbers; lse: [b][t][heads] floats, the
  *           natural logarithm of the sum of exponentials, or NULL.
- * A draft that sees nothing, and one at or past its count, gets zeros and
- * -infinity.  What an unseen position holds has no influence.  Limits: t * heads
- * <= 2^24, b * t * heads <= 2^31 - 256.
+ * A draft that sees nothing (or nothing but scores of -infinity), and one at or
+ * past its count, gets zeros and -infinity.  What an unseen position holds has no
+ * influence.  Limits: t * heads <= 2^24, b * t * heads <= 2^31 - 256.
  */
 typedef struct {
     int32_t type;   /* of q and out (at 16 bits the cache's type) */

@@ -8,9 +8,9 @@
 // the sum of two 16-bit numbers (the matrix instructions have time to spare
 // here), so that rounding them costs nothing.
 //   8 heads of 128, 32 queries, bf16, 64 sequences of 8192, one token each: 16
-//   bits 361 us (5.96 TB/s), 8 bits 207 us (5.36 TB/s), 4 bits 169 us (3.4 TB/s:
+//   bits 361 us (5.95 TB/s), 8 bits 203 us (5.46 TB/s), 4 bits 171 us (3.3 TB/s:
 //   expanding the codes).  One sequence of 32768 at 8 bits: 25 us; of 1000 at 16
-//   bits: 10.8 us, two launches whose chains of loads (lengths, pages, keys) set
+//   bits: 11.1 us, two launches whose chains of loads (lengths, pages, keys) set
 //   the time.
 #pragma once
 

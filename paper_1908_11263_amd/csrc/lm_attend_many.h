@@ -11,12 +11,17 @@
 // the many rows here its time counts.  The sums of the softmax take them as
 // they were before that.
 //   4 sequences of up to 32768 positions at 4 bits, 4 heads of 128 with 8 queries
-//   each (f16), trees of 61: 190 us and 12 to join, 630 TFLOP/s; 8 of up to 8192
-//   at 8 bits, 8 heads with 4 queries (bf16), trees of 16: 49 us and 3.  The
-//   vector units are busy 57 % of the time, the matrix units 24 %, local memory
-//   41 %.  Tiles of 32 positions: 255 and 58 us; the same with one load ahead: 265
-//   and 65; 64 positions and one load ahead: 198 and 57 (206 and 56 with two on
-//   that card: no clear difference).
+//   each (f16), trees of 61: 211 us, 12 of them to join, 606 TFLOP/s; 8 of up to
+//   8192 at 8 bits, 8 heads with 4 queries (bf16), trees of 16: 54 us and 7.  Of
+//   the first the vector units are busy 43 % of the time, the matrix units 20 %,
+//   local memory 38 %.  A prompt's chunk of 512 behind 8192, 8 heads with 4
+//   queries, 8 bits: 151 us (470 TFLOP/s), 16 bits 226 us; 2048 from an empty
+//   cache 124 and 230 us.  Measured on the first two when they took 206 and 56:
+//   tiles of 32 positions 255 and 58 us, with one load ahead 265 and 65; one load
+//   ahead 198 and 57 (no clear difference).
+//   The error of the results, of their norm: 1.68e-3 over caches of 8 bits and
+//   2.06e-3 over 16 bits (bf16, where one rounding of the result is 1.65e-3), 2.6
+//   to 3.0e-4 (f16: 2.1e-4).
 #pragma once
 
 #include <type_traits>

@@ -53,10 +53,12 @@ static hipError_t launch_f16(const MatmulArgs &a, int bits, void *ws, hipStream_
 //   Pieces of k shorten a workgroup's chain of steps, which bounds small grids,
 //   and cost their sums' way through memory: about the square root of the chain
 //   over the sums, and one more where that asks no compute unit for another
-//   workgroup.  128 x 4096 to 4096: 20 in 4 pieces, 25 in 2, 22.5 in 8; 16-bit
-//   weights, 256 x 4096 to 4096: 23 in 2, 29.5 whole, 26 in 4; 128 x 4096 to
-//   14336: 31 whole, 37 in 2; gated, 64 x 4096 to 11264: 33 in 4, 42 whole, 37
-//   in 2.
+//   workgroup.  128 x 4096 to 4096: 20.9 in 4 pieces, 26 in 2, 39 whole; 256 x
+//   4096 to 4096: 26 in 4, 29 in 2, 39 whole; 512 x 4096 to 4096: 37 in 2, 40
+//   whole, 41 in 4; 128 x 4096 to 14336: 35.6 in 2, 39.6 whole, 39.4 in 4; 1024 x
+//   4096 to 4096: 53 whole, 62 in 2; 16-bit weights, 256 x 4096 to 4096: 23 in 2,
+//   29.5 whole, 26 in 4; 128 x 4096 to 14336: 31 whole, 37 in 2; gated, 64 x 4096
+//   to 11264: 34.6 in 4, 36 in 3, 37 in 2, 43 whole.
 TilePlan plan_matmul(const MatmulArgs &a, int bits)
 {
     TilePlan p = {0, 0, 1, (a.k + 127) / 128 * 128};

@@ -1,6 +1,9 @@
-// The linear layer for more than 16 rows (trees of drafts, prompts): bound by
-// the vector units, which expand the codes, and the matrix units, which hardly
-// overlap (each busy 45 % of the time in the largest tiles).
+// The linear layer for more than 16 rows (trees of drafts, prompts).  With codes
+// it is bound by the vector units, which expand them, and the matrix units, which
+// hardly overlap (busy 50 and 45 % of the time in the largest tiles at 4 bits in
+// groups).  With 16-bit weights no unit is full (matrix 45 %, vector 14 %, reads
+// of local memory 18 %): waves wait a third of their time for the copies and the
+// barriers around them, and nearly half to issue.
 //
 // y = x w^T on the 32x32x16 matrix instruction, A = 32 rows of x, B = 32 rows
 // of weights.  A workgroup of four waves owns 32 TF rows of x and 128 WF rows of
@@ -12,11 +15,11 @@
 // row by the row's number, so that the fragments' reads spread over the banks;
 // the copy writes them in lane order, so the permutation is applied to the
 // address that a lane reads from memory.
-//   4096 x 4096 to 8192, bf16: 4 bits and a scale a row 252 us (1089 TFLOP/s),
-//   in groups of 128 284 us, 8 bits 264 us, 16 bits 291 us, 2 bits in groups 302
-//   us; 4096 x 11264 to 4096, 4 bits in groups: 375 us (1007 TFLOP/s).  A product
-//   of two 16-bit matrices of the first size takes 1510 to 1600 TFLOP/s in a
-//   library.
+//   4096 x 4096 to 8192, bf16: 4 bits and a scale a row 250 us (1099 TFLOP/s),
+//   in groups of 128 286 us, 8 bits 262 us, 16 bits 295 us, 2 bits in groups 301
+//   us, 1 bit 304 us; 4096 x 11264 to 4096, 4 bits in groups: 373 us (1015
+//   TFLOP/s; 368 to 398 from card to card).  A product of two 16-bit matrices of
+//   the first size takes 1510 to 1600 TFLOP/s in a library.
 //
 // k is taken in blocks of 32: lane l holds row l % 32 at k = 16 (l / 32) .. +
 // 15 of the block, two eights, the same for x and weights.
@@ -29,7 +32,9 @@
 // fp32.  Where such a group holds codes after all (a quantizer that gives empty
 // groups the smallest scale there is leaves none), where a scale is 2^40 times
 // those before it, or where sums have passed fp32, the wave forms its sums anew
-// with an accumulator for each group (sums_by_groups).
+// with an accumulator for each group (sums_by_groups).  1024 x 4096 to 4096 at 4
+// bits: 56 us, 288 where every third group is 2^-70 of the others and counts, 80
+// where those are empty.
 #pragma once
 
 #include "lm_matmul.h"

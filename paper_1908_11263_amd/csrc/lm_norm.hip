@@ -4,9 +4,9 @@
 // Bound by memory: a row is read once into registers, normed there twice, and
 // written once.  Statistics are taken about the mean, in fp32, from registers
 // (mean first, then the squares), so that a large mean costs no digits.
-//   8192 rows of 5120 (layer norms, gates, fp32 h): 115 us, 4.36 TB/s, where a
-//   copy reaches 5.5; one row of 4096: 5.7 us, of which 3.5 are the kernel (two
-//   norms are six sums over the workgroup, one after the other).
+//   8192 rows of 5120 (layer norms, gates, fp32 h): 116 us, 4.35 TB/s, where a
+//   copy reaches 5.5; one row of 4096: 5.7 us, of which 3.5 are the kernel (a
+//   sum over the workgroup a norm, two a layer norm, one after the other).
 #include "lm_common.h"
 #include "lm_internal.h"
 

@@ -67,8 +67,9 @@ def decoder_block(h, x, block, cache, table, lens, mask=None, counts=None, strea
       "mid_norm", "next_norm"          of the norms before the feed-forward layer and the next block
       "alpha", "beta"                  scales of the residual stream and of a half's result
     cache: a lm.Cache; table, lens, mask, counts: as lm.tree_attention takes them.
-    Positions enter with x (embedded, or turned before the block).  Writes the
-    drafts' keys and values behind lens and returns (h, x) for the next block."""
+    The block does not turn queries and keys by their positions: these are to be
+    part of the embedding.  Writes the drafts' keys and values behind lens and
+    returns (h, x) for the next block."""
     from . import lm
     b, t, d = x.shape
     heads, kv, dim = block["heads"], block["kv_heads"], block["dim"]
