@@ -178,6 +178,16 @@ float real(PyObject *o)
     return (float)v;
 }
 
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) {
+        PyErr_Clear();
+        bad("True or False was expected");
+    }
+    return v != 0;
+}
+
 template <class F>
 PyObject *guarded(F f)
 {
@@ -234,7 +244,7 @@ PyObject *matmul(PyObject *, PyObject *const *a, Py_ssize_t n)
             bad("w must be contiguous rows of " + std::to_string(k) + " channels of " + std::to_string(bits) + " bits");
         at.same(w);
         const int64_t rows = w.size(0);
-        s.gated = PyObject_IsTrue(a[6]) ? 1 : 0;
+        s.gated = truth(a[6]) ? 1 : 0;
         if (s.gated && rows % 2)
             bad("a gated layer has an even number of rows");
         const int64_t m = s.gated ? rows / 2 : rows;
@@ -325,7 +335,7 @@ PyObject *norm_residual(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.d = int32_of(d, "the number of channels");
         s.r = int32_of(rows_of(h), "the number of rows");
         s.norm = (int32_t)number(a[2]);
-        s.post = PyObject_IsTrue(a[3]) ? 1 : 0;
+        s.post = truth(a[3]) ? 1 : 0;
         s.gates = 0;
         s.alpha = real(a[9]);
         s.beta = real(a[10]);
@@ -479,7 +489,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         } else {
             made = make(q.sizes(), q, q.scalar_type());
         }
-        const bool want = PyObject_IsTrue(a[8]);
+        const bool want = truth(a[8]);
         if (want)
             lse = make(q.sizes().slice(0, 3), q, at::kFloat);
         const size_t size = g_lib.tree_attention_workspace(&s, &cache.c);
@@ -575,7 +585,7 @@ PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n)
         arguments(n, 10);
         Py_XDECREF(g_error);
         g_error = own(a[0]);
-        g_gpu = PyObject_IsTrue(a[1]);
+        g_gpu = truth(a[1]);
         void *p[8];
         for (int i = 0; i < 8; ++i)
             p[i] = PyLong_AsVoidPtr(a[2 + i]);

@@ -44,3 +44,13 @@ def test_gradients_are_refused(lm):
             with torch.no_grad(), pytest.raises((ValueError, RuntimeError)) as e:
                 f(**a)
             assert "gradient" not in str(e.value)
+
+
+def test_flags_without_a_truth_value(lm):
+    """A flag that is neither true nor false is refused, not taken for true with the error left behind."""
+    (matmul, a, _), (_, b, _), (norm, c, _), (attend, d, _) = list(calls(lm))[:4]
+    neither = torch.zeros(2)
+    for f, args in ((matmul, dict(a, residual=None, gated=neither)), (norm, dict(c, post=neither)),
+                    (attend, dict(d, want_lse=neither))):
+        with pytest.raises(ValueError, match="True or False"):
+            f(**args)
