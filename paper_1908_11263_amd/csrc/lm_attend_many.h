@@ -19,9 +19,9 @@
 //   cache 124 and 230 us.  Measured on the first two when they took 206 and 56:
 //   tiles of 32 positions 255 and 58 us, with one load ahead 265 and 65; one load
 //   ahead 198 and 57 (no clear difference).
-//   The error of the results, of their norm: 1.68e-3 over caches of 8 bits and
-//   2.06e-3 over 16 bits (bf16, where one rounding of the result is 1.65e-3), 2.6
-//   to 3.0e-4 (f16: 2.1e-4).
+//   The error of the results, of their norm: 1.7e-3 over caches of 8 bits and up to
+//   2.3e-3 over 16 bits (bf16, where one rounding of the result is 1.65e-3), 2.6 to
+//   3.4e-4 (f16: 2.1e-4).
 #pragma once
 
 #include <type_traits>
